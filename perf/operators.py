@@ -183,7 +183,7 @@ def prepare(case, seed):
         n, rows = case["n"], case["rows"]
         s["ids"] = _listed(gen, n, rows) if case["listed"] else None
         s["codes"] = torch.zeros((n, 2 * hidden), dtype=torch.uint8, device="cuda")
-        s["scales"] = torch.zeros((n, 2 * heads), dtype=torch.uint8, device="cuda")
+        s["scales"] = torch.zeros((n, heads, 2), dtype=torch.uint8, device="cuda")
         if case["op"] == "write":
             s["K"], s["V"] = _kv(gen, rows, hidden, dtype)
         else:
@@ -214,7 +214,7 @@ def prepare(case, seed):
 # ----------------------------------------------------------------------------------------- plain forms
 
 def _quantise(x, fmt):
-    """Codes and scale bytes of rows: blocks of 32 values, code = round(x / 2^e) (to nearest, ties to even) with the smallest
+    """Codes and scale bytes ([rows, heads, 2]) of K | V rows: blocks of 32 values, code = round(x / 2^e) (to nearest, ties to even) with the smallest
     e that keeps the block within the format, byte = e + 127. Everything but that rounding is exact."""
     x = x.float().unflatten(1, (-1, HEAD))
     top = x.abs().amax(2)
@@ -224,11 +224,11 @@ def _quantise(x, fmt):
     byte = torch.where(top > 0, (e + 127).clamp(0, 254), 0)
     y = x * torch.exp2((127 - byte).double()).float()[..., None]
     codes = y.to(torch.float8_e4m3fn) if fmt == "e4m3" else y.round().to(torch.int8)
-    return codes.view(torch.uint8).flatten(1), byte.to(torch.uint8)
+    return codes.view(torch.uint8).flatten(1), byte.to(torch.uint8).unflatten(1, (2, -1)).transpose(1, 2).contiguous()
 
 
 def _values(codes, scales, fmt):
-    """What rows of the store stand for, in 32 bits."""
+    """What the K or V parts of rows stand for, in 32 bits."""
     c = (codes.view(torch.float8_e4m3fn) if fmt == "e4m3" else codes.view(torch.int8)).float()
     return (c.unflatten(-1, (-1, HEAD)) * scales.view(torch.float8_e8m0fnu).float()[..., None]).flatten(-2)
 
@@ -243,18 +243,18 @@ def _plain(s):
     dtype, hidden = DTYPES[s["dtype"]], s["hidden"]
     if s["op"] == "read":
         at = slice(0, s["rows"]) if s["ids"] is None else s["ids"].long()
-        kv = _values(s["codes"][at], s["scales"][at], s["fmt"]).to(dtype)
-        return {"K": kv[:, :hidden].contiguous(), "V": kv[:, hidden:].contiguous()}
+        return {"K": _values(s["codes"][at, :hidden], s["scales"][at, :, 0], s["fmt"]).to(dtype),
+                "V": _values(s["codes"][at, hidden:], s["scales"][at, :, 1], s["fmt"]).to(dtype)}
     if s["op"] == "attn":
         heads = hidden // HEAD
         nbr = s["nbr"].clamp(min=0)
-        k = _values(s["codes"][:, :hidden][nbr], s["scales"][:, :heads][nbr], s["fmt"]).unflatten(2, (heads, HEAD))
+        k = _values(s["codes"][:, :hidden][nbr], s["scales"][..., 0][nbr], s["fmt"]).unflatten(2, (heads, HEAD))
         score = (k * s["Q"].float().view(-1, 1, heads, HEAD)).sum(3) * HEAD ** -0.5 + s["bias"].t()[s["rel"]]
         del k
         score = torch.where((s["nbr"] >= 0)[..., None], score, -math.inf)
         p = torch.exp(score - score.amax(1, keepdim=True))
         p = p / p.sum(1, keepdim=True)
-        v = _values(s["codes"][:, hidden:][nbr], s["scales"][:, heads:][nbr], s["fmt"]).unflatten(2, (heads, HEAD))
+        v = _values(s["codes"][:, hidden:][nbr], s["scales"][..., 1][nbr], s["fmt"]).unflatten(2, (heads, HEAD))
         return {"A": (p[..., None] * v).sum(1).flatten(1).to(dtype)}
     x = s["S"].float()
     mine = s["adapter"][:, None] == torch.arange(s["adapters"], device="cuda", dtype=torch.int32)
@@ -328,9 +328,8 @@ def _exact_write(s):
         else:
             y = torch.round(y)
         at = torch.arange(s["rows"], device="cuda") if s["ids"] is None else s["ids"].long()
-        heads = d // HEAD
         codes[at, part * d:(part + 1) * d] = y.flatten(1)
-        scales[at, part * heads:(part + 1) * heads] = scale
+        scales[at, :, part] = scale
     return {"codes": codes, "scales": scales}
 
 
@@ -342,7 +341,7 @@ def _exact_values(s, part, rows):
     else:
         e, m = (c >> 3) & 15, (c & 7).double()
         v = torch.where(e > 0, (8 + m) * torch.exp2((e - 10).double()), m * 2.0 ** -9) * torch.where(c < 128, 1.0, -1.0)
-    size = torch.exp2(s["scales"][rows, part * heads:(part + 1) * heads].double() - 127)
+    size = torch.exp2(s["scales"][rows, :, part].double() - 127)
     return v.view(-1, heads, HEAD) * size[..., None]
 
 
