@@ -35,6 +35,15 @@ typedef struct dg4_graph dg4_graph;
 
 typedef enum { DG4_F32 = 0, DG4_BF16 = 1 } dg4_dtype;
 
+/* Element format of a K|V store in 8 bits (dg4_kv8_write) */
+typedef enum {
+    DG4_KV_E4M3 = 0,        /* floating: 4 exponent and 3 mantissa bits, largest 448; relative  */
+                            /* error of a value at most 2^-4 down to 2^-14 of its block's range */
+    DG4_KV_INT8 = 1         /* whole numbers -127 .. 127; error at most 1/127 of the block's    */
+                            /* largest magnitude (or 2^-128), four times less on average than   */
+                            /* e4m3's                                                           */
+} dg4_kv_format;
+
 typedef enum {
     DG4_OK = 0,
     DG4_EINVAL = -1,        /* null pointer, negative size, bad flag or bad config field   */
@@ -302,6 +311,48 @@ int dg4_ffn_fwd(const dg4_layer_cfg* cfg, const void* S, int64_t row_begin, int6
 int dg4_sparse_attn_fwd(const dg4_layer_cfg* cfg, dg4_graph* g, int64_t row_begin, int64_t row_end,
                         const void* Q, const void* K, const void* V, const float* rel_bias,
                         void* A, void* stream);
+
+/*
+ * The K|V store in 8 bits: the historical K and V rows (Section 3.4) at half the bytes of bfloat16, a
+ * quarter of float. Store row u, n_store rows, both arrays device memory of the caller:
+ *   codes  uint8 [n_store, 2*hidden]     K of all heads | V of all heads, in the element format
+ *   scales uint8 [n_store, heads, 2]     for K and V of each head a power of two, as exponent + 127
+ * A value is code * 2^(scale - 127). Writing quantises by blocks of one head (32 features): the scale
+ * is the smallest power of two with which the block's largest magnitude stays within the format's
+ * largest code (448 or 127; not below 2^-127), a value divided by it is rounded to the nearest code,
+ * ties to even. Nothing else is rounded. A block that holds an infinity or a NaN gets scale 255 and
+ * reads as NaN.
+ *   dg4_kv8_write: rows [row_begin, row_end) of K and V [*, hidden] (cfg->dtype) into the store; row r
+ *   goes to store row ids[r], or to row r without ids (then row_end <= n_store). Entries of ids outside
+ *   [0, n_store) are skipped (-1: a padded row); the others are distinct, and which of two rows with
+ *   one id remains is not defined. Store rows that are not named stay as they are.
+ */
+int dg4_kv8_write(const dg4_layer_cfg* cfg, int32_t format, const void* K, const void* V,
+                  int64_t row_begin, int64_t row_end, const int32_t* ids /* nullable, device */,
+                  uint8_t* codes, uint8_t* scales, int64_t n_store, void* stream);
+
+/*
+ * Rows [row_begin, row_end) of K and V [*, hidden] from the store: row r is store row ids[r] (any
+ * number of times the same), or row r without ids. Rows whose id is outside [0, n_store) stay as they
+ * are. Exact in float and bfloat16 (a code has at most 8 significant bits) as far as the type reaches.
+ */
+int dg4_kv8_read(const dg4_layer_cfg* cfg, int32_t format, const uint8_t* codes, const uint8_t* scales,
+                 int64_t n_store, const int32_t* ids /* nullable, device */,
+                 int64_t row_begin, int64_t row_end, void* K, void* V, void* stream);
+
+/*
+ * dg4_sparse_attn_fwd over a store in 8 bits (graph's n_nodes rows, row = node id; the gate's own row
+ * among them): rows [row_begin, row_end) of Q and A, row r the gate ids[r] (rows with an id outside
+ * [0, n_nodes) stay as they are), or gate r without ids (then row_end <= n_nodes). Scores, softmax and
+ * sums in fp32, one rounding to cfg->dtype. rel_bias = -infinity leaves a head's sources of that
+ * relation out: what the store holds for them is not looked at, and a head whose sources are all left
+ * out gives zeros. The result of a row does not depend on which rows a call covers. The graph's
+ * neighbour tables must be on the current device (EINVAL otherwise).
+ */
+int dg4_sparse_attn_kv8_fwd(const dg4_layer_cfg* cfg, int32_t format, dg4_graph* g,
+                            int64_t row_begin, int64_t row_end, const int32_t* ids /* nullable, device */,
+                            const void* Q, const uint8_t* codes, const uint8_t* scales,
+                            const float* rel_bias, void* A, void* stream);
 
 /*
  * The level sweep of the updating strategy (Section 3.4, Algorithm 2 with

@@ -29,6 +29,7 @@ ARRAYS = {"level": (0, np.int32), "order": (1, np.int32), "level_ptr": (2, np.in
           "pair_order": (10, np.int32), "pair_tile_ptr": (11, np.int64),
           "cone_root": (12, np.int32), "cone_group_level": (13, np.int32), "cone_group_ptr": (14, np.int64),
           "stage": (15, np.int32), "copy_of": (16, np.int32), "last_copy": (17, np.int32)}
+KV_FORMATS = {"e4m3": 0, "int8": 1}
 STATUS = {0: "OK", -1: "EINVAL", -2: "ERANGE", -3: "EFANIN", -4: "ECYCLE", -5: "EHINT",
           -6: "EUNSUPPORTED", -7: "ENOMEM", -8: "EWORKSPACE", -9: "EHIP", -10: "EABORTED"}
 
@@ -125,6 +126,12 @@ def lib():
         L.dg4_struct_encode.argtypes = [ctypes.POINTER(_Cfg), _P, _P, _P, _P, _P]
         L.dg4_sparse_attn_fwd.restype = ctypes.c_int
         L.dg4_sparse_attn_fwd.argtypes = [ctypes.POINTER(_Cfg), _P, _I64, _I64, _P, _P, _P, _P, _P, _P]
+        L.dg4_kv8_write.restype = ctypes.c_int
+        L.dg4_kv8_write.argtypes = [ctypes.POINTER(_Cfg), _I32, _P, _P, _I64, _I64, _P, _P, _P, _I64, _P]
+        L.dg4_kv8_read.restype = ctypes.c_int
+        L.dg4_kv8_read.argtypes = [ctypes.POINTER(_Cfg), _I32, _P, _P, _I64, _P, _I64, _I64, _P, _P, _P]
+        L.dg4_sparse_attn_kv8_fwd.restype = ctypes.c_int
+        L.dg4_sparse_attn_kv8_fwd.argtypes = [ctypes.POINTER(_Cfg), _I32, _P, _I64, _I64, _P, _P, _P, _P, _P, _P, _P]
         L.dg4_layer_fwd.restype = ctypes.c_int
         L.dg4_layer_fwd.argtypes = [ctypes.POINTER(_Cfg), _P, _P, ctypes.POINTER(_P), _I32, _I32, _P, _P, _I64, _P]
         L.dg4_sweep_elapsed_ms.restype = ctypes.c_int
@@ -337,6 +344,67 @@ def dg4_sparse_attn_fwd(cfg: LayerConfig, g: Graph, Q, K, V, rel_bias, A, row_be
     rc = lib().dg4_sparse_attn_fwd(ctypes.byref(c), g.handle, row_begin, row_end, Q.data_ptr(), K.data_ptr(),
                                    V.data_ptr(), rel_bias.data_ptr(), A.data_ptr(), _stream())
     _check(rc, "dg4_sparse_attn_fwd")
+
+
+def _tensors(where: str, *wanted):
+    """(tensor, element type, columns) each: contiguous rows on the current device, or EINVAL."""
+    import torch
+    dev = torch.cuda.current_device()
+    for t, dtype, cols in wanted:
+        if t.dtype != dtype or not t.is_cuda or t.get_device() != dev or not t.is_contiguous() or \
+           (cols is not None and (t.dim() < 2 or t.shape[0] and t.numel() // t.shape[0] != cols)):
+            raise DG4Error(-1, where)
+
+
+def _store_call(where: str, cfg: LayerConfig, fmt: str, codes, scales, ids, rows, row_begin, row_end, n_store):
+    """What the calls on a K|V store in 8 bits check and fill in: (format, end of the range, store rows, ids)."""
+    import torch
+    if fmt not in KV_FORMATS or cfg.dtype not in ("f32", "bf16") or any(t.shape[0] != rows[0].shape[0] for t in rows):
+        raise DG4Error(-1, where)
+    td = torch.float32 if cfg.dtype == "f32" else torch.bfloat16
+    _tensors(where, (codes, torch.uint8, 2 * cfg.hidden), (scales, torch.uint8, 2 * cfg.heads), *((t, td, cfg.hidden) for t in rows))
+    have = rows[0].shape[0]
+    if ids is not None:
+        _tensors(where, (ids, torch.int32, None))
+        have = min(have, ids.numel())
+    n_store = min(codes.shape[0], scales.shape[0]) if n_store is None else n_store
+    row_end = rows[0].shape[0] if row_end is None else row_end
+    if row_end > have or n_store > min(codes.shape[0], scales.shape[0]):
+        raise DG4Error(-1, where)
+    return KV_FORMATS[fmt], row_end, n_store, ids.data_ptr() if ids is not None else None
+
+
+def dg4_kv8_write(cfg: LayerConfig, fmt: str, K, V, codes, scales, ids=None, row_begin=0, row_end=None):
+    """Rows [row_begin,row_end) of K and V into the 8-bit store (fmt "e4m3" | "int8"): codes uint8 [n, 2*hidden] and
+    scales uint8 [n, heads, 2] in place. ids: int32 store row of each row (outside the store: skipped), else the row itself."""
+    f, row_end, n, ip = _store_call("dg4_kv8_write", cfg, fmt, codes, scales, ids, (K, V), row_begin, row_end, None)
+    c = cfg.c()
+    rc = lib().dg4_kv8_write(ctypes.byref(c), f, K.data_ptr(), V.data_ptr(), row_begin, row_end, ip, codes.data_ptr(),
+                             scales.data_ptr(), n, _stream())
+    _check(rc, "dg4_kv8_write")
+
+
+def dg4_kv8_read(cfg: LayerConfig, fmt: str, codes, scales, K, V, ids=None, row_begin=0, row_end=None):
+    """Rows [row_begin,row_end) of K and V, in place, from the 8-bit store; ids as in dg4_kv8_write."""
+    f, row_end, n, ip = _store_call("dg4_kv8_read", cfg, fmt, codes, scales, ids, (K, V), row_begin, row_end, None)
+    c = cfg.c()
+    rc = lib().dg4_kv8_read(ctypes.byref(c), f, codes.data_ptr(), scales.data_ptr(), n, ip, row_begin, row_end,
+                            K.data_ptr(), V.data_ptr(), _stream())
+    _check(rc, "dg4_kv8_read")
+
+
+def dg4_sparse_attn_kv8_fwd(cfg: LayerConfig, fmt: str, g: Graph, Q, codes, scales, rel_bias, A, ids=None, row_begin=0,
+                            row_end=None):
+    """Cone attention over the 8-bit store (row = node id). ids: int32 gate of each row of Q and A, else the row itself."""
+    import torch
+    f, row_end, _, ip = _store_call("dg4_sparse_attn_kv8_fwd", cfg, fmt, codes, scales, ids, (Q, A), row_begin, row_end, g.n)
+    _tensors("dg4_sparse_attn_kv8_fwd", (rel_bias, torch.float32, 4))
+    if rel_bias.shape[0] != cfg.heads:
+        raise DG4Error(-1, "dg4_sparse_attn_kv8_fwd")
+    c = cfg.c()
+    rc = lib().dg4_sparse_attn_kv8_fwd(ctypes.byref(c), f, g.handle, row_begin, row_end, ip, Q.data_ptr(), codes.data_ptr(),
+                                       scales.data_ptr(), rel_bias.data_ptr(), A.data_ptr(), _stream())
+    _check(rc, "dg4_sparse_attn_kv8_fwd")
 
 
 def dg4_layer_fwd(cfg: LayerConfig, g: Graph, X, weights, Hout, level_begin=0, level_end=None, workspace=None):

@@ -154,6 +154,18 @@ SweepEvents& sweep_events() { static SweepEvents e; return e; }
 // rows are read and written as 16-byte pieces
 template <typename... P> bool aligned16(P... ptrs) { return (((uintptr_t)ptrs | ...) & 15) == 0; }
 
+// What the calls on a K|V store in 8 bits share: configuration, the store's two arrays, the range of rows
+int check_kv8(const dg4_layer_cfg* cfg, int32_t format, const int32_t* ids, const uint8_t* codes, const uint8_t* scales,
+              int64_t n_store, int64_t row_begin, int64_t row_end)
+{
+    const int rc = check_cfg(cfg, false);
+    if (rc != DG4_OK) return rc;
+    if (format != DG4_KV_E4M3 && format != DG4_KV_INT8) return DG4_EINVAL;
+    if (!codes || !scales || !aligned16(codes, scales) || ((uintptr_t)ids & 3)) return DG4_EINVAL;
+    if (n_store < 0 || row_begin < 0 || row_end < row_begin || (!ids && row_end > n_store)) return DG4_EINVAL;
+    return DG4_OK;
+}
+
 }  // namespace
 
 extern "C" const char* dg4_strerror(int status)
@@ -309,6 +321,63 @@ extern "C" int dg4_sparse_attn_fwd(const dg4_layer_cfg* cfg, dg4_graph* g, int64
     a.a = A; a.a_stride = d;
     a.row_begin = row_begin; a.row_end = row_end;
     HIPCHK(dg4_launch_attn(cfg->dtype, d, a, (hipStream_t)stream));
+    return DG4_OK;
+}
+
+extern "C" int dg4_kv8_write(const dg4_layer_cfg* cfg, int32_t format, const void* K, const void* V,
+                             int64_t row_begin, int64_t row_end, const int32_t* ids,
+                             uint8_t* codes, uint8_t* scales, int64_t n_store, void* stream)
+{
+    const int rc = check_kv8(cfg, format, ids, codes, scales, n_store, row_begin, row_end);
+    if (rc != DG4_OK) return rc;
+    if (!K || !V || !aligned16(K, V)) return DG4_EINVAL;
+    if (row_end == row_begin || n_store == 0) return DG4_OK;
+    dg4_kv8_args a{};
+    a.k = K; a.v = V;
+    a.codes = codes; a.scales = scales; a.n_store = n_store;
+    a.ids = ids; a.row_begin = row_begin; a.row_end = row_end;
+    HIPCHK(dg4_launch_kv8_write(cfg->dtype, format, cfg->hidden, a, (hipStream_t)stream));
+    return DG4_OK;
+}
+
+extern "C" int dg4_kv8_read(const dg4_layer_cfg* cfg, int32_t format, const uint8_t* codes, const uint8_t* scales,
+                            int64_t n_store, const int32_t* ids, int64_t row_begin, int64_t row_end,
+                            void* K, void* V, void* stream)
+{
+    const int rc = check_kv8(cfg, format, ids, codes, scales, n_store, row_begin, row_end);
+    if (rc != DG4_OK) return rc;
+    if (!K || !V || !aligned16(K, V)) return DG4_EINVAL;
+    if (row_end == row_begin || n_store == 0) return DG4_OK;
+    dg4_kv8_args a{};
+    a.k_out = K; a.v_out = V;
+    a.codes = const_cast<uint8_t*>(codes); a.scales = const_cast<uint8_t*>(scales); a.n_store = n_store;
+    a.ids = ids; a.row_begin = row_begin; a.row_end = row_end;
+    HIPCHK(dg4_launch_kv8_read(cfg->dtype, format, cfg->hidden, a, (hipStream_t)stream));
+    return DG4_OK;
+}
+
+extern "C" int dg4_sparse_attn_kv8_fwd(const dg4_layer_cfg* cfg, int32_t format, dg4_graph* g,
+                                       int64_t row_begin, int64_t row_end, const int32_t* ids,
+                                       const void* Q, const uint8_t* codes, const uint8_t* scales,
+                                       const float* rel_bias, void* A, void* stream)
+{
+    if (!g) return DG4_EINVAL;
+    int rc = check_kv8(cfg, format, ids, codes, scales, g->n, row_begin, row_end);
+    if (rc != DG4_OK) return rc;
+    if (!Q || !rel_bias || !A || !aligned16(Q, A) || ((uintptr_t)rel_bias & 3) || g->hops != cfg->hops) return DG4_EINVAL;
+    if (row_end == row_begin || g->n == 0) return DG4_OK;
+    rc = dg4_graph_ensure_device(g);
+    if (rc != DG4_OK) return rc;
+    int dev = -1;
+    if (hipGetDevice(&dev) != hipSuccess) return DG4_EHIP;
+    if (dev != g->device) return DG4_EINVAL;
+    dg4_kv8_attn_args a{};
+    a.q = Q; a.a = A;
+    a.codes = codes; a.scales = scales; a.n = g->n;
+    a.rel_bias = rel_bias;
+    a.ell = g->d_ell_id; a.ell_w = g->ell_w;
+    a.ids = ids; a.row_begin = row_begin; a.row_end = row_end;
+    HIPCHK(dg4_launch_kv8_attn(cfg->dtype, format, cfg->hidden, a, (hipStream_t)stream));
     return DG4_OK;
 }
 

@@ -344,6 +344,28 @@ struct dg4_bulk_args {
 int dg4_launch_pack_w32(const void* w, int ld, void* packed, hipStream_t s);   // [256, 768] weights, row stride ld
 int dg4_launch_bulk_proj(const dg4_bulk_args& a, hipStream_t s);
 
+// ---- the K|V store in 8 bits (dg4_kv8.hip) ----
+struct dg4_kv8_args {
+    const void* k; const void* v;          // write: [*, d] rows
+    void* k_out; void* v_out;              // read: [*, d] rows
+    uint8_t* codes;                        // [n_store, 2d] K | V
+    uint8_t* scales;                       // [n_store, heads, 2] biased exponents of K and V
+    const int32_t* ids;                    // nullable: store row of row r is ids[r], else r; none if outside [0, n_store)
+    int64_t n_store;
+    int64_t row_begin, row_end;
+};
+struct dg4_kv8_attn_args {
+    const void* q; void* a;                // [*, d] rows
+    const uint8_t* codes; const uint8_t* scales; int64_t n;
+    const float* rel_bias;                 // [heads, 4]
+    const uint32_t* ell; int ell_w;        // neighbour rows by node id
+    const int32_t* ids;                    // nullable: the gate of row r is ids[r], else r; none if outside [0, n)
+    int64_t row_begin, row_end;
+};
+int dg4_launch_kv8_write(int dtype, int format, int hidden, const dg4_kv8_args& a, hipStream_t s);
+int dg4_launch_kv8_read(int dtype, int format, int hidden, const dg4_kv8_args& a, hipStream_t s);
+int dg4_launch_kv8_attn(int dtype, int format, int hidden, const dg4_kv8_attn_args& a, hipStream_t s);
+
 // Every kernel takes its argument block by value: plain data of pointer alignment, well inside the
 // kernel-argument segment (4 KB), value-initialised by every caller before the fields are set.
 #define DG4_CHECK_KERNEL_ARGS(S) \
@@ -355,5 +377,7 @@ DG4_CHECK_KERNEL_ARGS(dg4_sweep_args);
 DG4_CHECK_KERNEL_ARGS(dg4_flow_args);
 DG4_CHECK_KERNEL_ARGS(dg4_bulk_args);
 DG4_CHECK_KERNEL_ARGS(dg4_heads_args);
+DG4_CHECK_KERNEL_ARGS(dg4_kv8_args);
+DG4_CHECK_KERNEL_ARGS(dg4_kv8_attn_args);
 DG4_CHECK_KERNEL_ARGS(dg4_heads_pack_args);
 #undef DG4_CHECK_KERNEL_ARGS
