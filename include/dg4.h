@@ -287,6 +287,32 @@ int dg4_qkv_proj_static(const dg4_layer_cfg* cfg, const void* S, int64_t row_beg
                         const void* Wqkv, void* Q, void* K, void* V, void* stream);
 
 /*
+ * The projection with low-rank adapters beside it, for rows of many circuits at once:
+ *   [Q | K | V][r] = S[r] Wqkv + gain[a] (S[r] Down_a) Up_a,  a = adapter[r]
+ * Down_a [hidden, rank], Up_a [rank, 3*hidden], rank 1..DG4_MAX_RANK (adapters of smaller rank are
+ * padded with zeros). dg4_lora_pack lays the weights out once in matrix-core operand order:
+ *   Wqkv as in dg4_qkv_proj; Down [n_adapters, hidden, rank], Up [n_adapters, rank, 3*hidden] device,
+ *   row-major, cfg->dtype; gain device float [n_adapters], null: 1 for all. n_adapters = 0 is allowed
+ *   (rank, Down, Up, gain are not looked at then). packed: dg4_lora_packed_bytes, 256-byte aligned
+ *   (EWORKSPACE otherwise). cfg: hidden, heads, dtype are used.
+ * dg4_qkv_proj_lora reads `packed` as a dg4_lora_pack of the same cfg, n_adapters and rank left it (any
+ * number of calls and streams at once may share it) for rows [row_begin, row_end) of S; adapter: device
+ * int32, one of every row of S, in any order (runs of equal ones cost least); a row whose adapter is
+ * outside [0, n_adapters), or any row where adapter is null, gets S[r] Wqkv alone. Q, K, V as in
+ * dg4_qkv_proj; they may not alias S. fp32 accumulation, one rounding to cfg->dtype at the end (S Down
+ * is carried in at least 16 significant bits in bfloat16). A row's result depends on nothing but the row,
+ * its adapter and Wqkv. Allocates nothing, one launch.
+ */
+#define DG4_MAX_RANK 64
+int64_t dg4_lora_packed_bytes(const dg4_layer_cfg* cfg, int32_t n_adapters, int32_t rank);
+int dg4_lora_pack(const dg4_layer_cfg* cfg, const void* Wqkv, int32_t n_adapters, int32_t rank,
+                  const void* Down, const void* Up, const float* gain /* nullable */,
+                  void* packed, int64_t packed_bytes, void* stream);
+int dg4_qkv_proj_lora(const dg4_layer_cfg* cfg, const void* packed, int64_t packed_bytes,
+                      int32_t n_adapters, int32_t rank, const void* S, int64_t row_begin, int64_t row_end,
+                      const int32_t* adapter /* nullable */, void* Q, void* K, void* V, void* stream);
+
+/*
  * The position-wise feed-forward sub-block that follows the attention sub-block in the
  * transformer layer (Section 3.5: the attention module is replaced, the rest of the transformer
  * structure is kept), for rows [row_begin, row_end) of S:

@@ -11,4 +11,5 @@ from .binding import (DG4Error, Graph, LayerConfig, dg4_build_levels, dg4_build_
                       dg4_qkv_proj_static, dg4_static_scratch_bytes,
                       dg4_ffn_fwd, dg4_ffn_workspace_bytes,
                       dg4_kv8_read, dg4_kv8_write, dg4_sparse_attn_kv8_fwd,
+                      LoraWeights, dg4_lora_pack, dg4_lora_packed_bytes, dg4_qkv_proj_lora,
                       dg4_sparse_attn_fwd, dg4_struct_encode, lib, library_path)

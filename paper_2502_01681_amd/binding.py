@@ -126,6 +126,12 @@ def lib():
         L.dg4_struct_encode.argtypes = [ctypes.POINTER(_Cfg), _P, _P, _P, _P, _P]
         L.dg4_sparse_attn_fwd.restype = ctypes.c_int
         L.dg4_sparse_attn_fwd.argtypes = [ctypes.POINTER(_Cfg), _P, _I64, _I64, _P, _P, _P, _P, _P, _P]
+        L.dg4_lora_packed_bytes.restype = _I64
+        L.dg4_lora_packed_bytes.argtypes = [ctypes.POINTER(_Cfg), _I32, _I32]
+        L.dg4_lora_pack.restype = ctypes.c_int
+        L.dg4_lora_pack.argtypes = [ctypes.POINTER(_Cfg), _P, _I32, _I32, _P, _P, _P, _P, _I64, _P]
+        L.dg4_qkv_proj_lora.restype = ctypes.c_int
+        L.dg4_qkv_proj_lora.argtypes = [ctypes.POINTER(_Cfg), _P, _I64, _I32, _I32, _P, _I64, _I64, _P, _P, _P, _P, _P]
         L.dg4_kv8_write.restype = ctypes.c_int
         L.dg4_kv8_write.argtypes = [ctypes.POINTER(_Cfg), _I32, _P, _P, _I64, _I64, _P, _P, _P, _I64, _P]
         L.dg4_kv8_read.restype = ctypes.c_int
@@ -354,6 +360,77 @@ def _tensors(where: str, *wanted):
         if t.dtype != dtype or not t.is_cuda or t.get_device() != dev or not t.is_contiguous() or \
            (cols is not None and (t.dim() < 2 or t.shape[0] and t.numel() // t.shape[0] != cols)):
             raise DG4Error(-1, where)
+
+
+@dataclass
+class LoraWeights:
+    """Shared projection and adapters in matrix-core operand order (dg4_lora_pack); read only from then on."""
+    packed: object               # uint8 device tensor
+    n_adapters: int
+    rank: int
+    hidden: int
+    dtype: str
+
+
+def dg4_lora_packed_bytes(cfg: LayerConfig, n_adapters: int, rank: int) -> int:
+    c = cfg.c()
+    r = lib().dg4_lora_packed_bytes(ctypes.byref(c), n_adapters, rank)
+    if r < 0:
+        raise DG4Error(int(r), "dg4_lora_packed_bytes")
+    return int(r)
+
+
+def dg4_lora_pack(cfg: LayerConfig, Wqkv, Down=None, Up=None, gain=None) -> LoraWeights:
+    """Wqkv [hidden, 3*hidden], Down [n_adapters, hidden, rank], Up [n_adapters, rank, 3*hidden], gain float [n_adapters]
+    (None: 1); without Down and Up the projection alone."""
+    import torch
+    where = "dg4_lora_pack"
+    if cfg.dtype not in ("f32", "bf16") or (Down is None) != (Up is None):
+        raise DG4Error(-1, where)
+    td = torch.float32 if cfg.dtype == "f32" else torch.bfloat16
+    _tensors(where, (Wqkv, td, 3 * cfg.hidden))
+    n, rank = (0, 1) if Down is None else (Down.shape[0], Down.shape[-1])
+    if n:
+        _tensors(where, (Down, td, None), (Up, td, None))
+        if tuple(Down.shape) != (n, cfg.hidden, rank) or tuple(Up.shape) != (n, rank, 3 * cfg.hidden):
+            raise DG4Error(-1, where)
+        if gain is not None:
+            _tensors(where, (gain, torch.float32, None))
+            if gain.numel() != n:
+                raise DG4Error(-1, where)
+    if Wqkv.shape[0] != cfg.hidden:
+        raise DG4Error(-1, where)
+    packed = _ws(dg4_lora_packed_bytes(cfg, n, rank), Wqkv)
+    c = cfg.c()
+    rc = lib().dg4_lora_pack(ctypes.byref(c), Wqkv.data_ptr(), n, rank, Down.data_ptr() if n else None,
+                             Up.data_ptr() if n else None, gain.data_ptr() if n and gain is not None else None,
+                             packed.data_ptr(), packed.numel(), _stream())
+    _check(rc, where)
+    return LoraWeights(packed, n, rank, cfg.hidden, cfg.dtype)
+
+
+def dg4_qkv_proj_lora(cfg: LayerConfig, weights: LoraWeights, S, adapter, Q, K, V, row_begin=0, row_end=None):
+    """Q, K, V rows [row_begin,row_end) = S rows x Wqkv + what the adapter of each row adds (int32, one of every row of S;
+    None or outside [0, n_adapters): nothing). In place."""
+    import torch
+    where = "dg4_qkv_proj_lora"
+    if cfg.dtype != weights.dtype or cfg.hidden != weights.hidden:
+        raise DG4Error(-1, where)
+    td = torch.float32 if cfg.dtype == "f32" else torch.bfloat16
+    _tensors(where, (S, td, cfg.hidden), (Q, td, cfg.hidden), (K, td, cfg.hidden), (V, td, cfg.hidden))
+    have = min(S.shape[0], Q.shape[0], K.shape[0], V.shape[0])
+    if adapter is not None:
+        _tensors(where, (adapter, torch.int32, None))
+        have = min(have, adapter.numel())
+    row_end = S.shape[0] if row_end is None else row_end
+    if row_end > have:
+        raise DG4Error(-1, where)
+    c = cfg.c()
+    rc = lib().dg4_qkv_proj_lora(ctypes.byref(c), weights.packed.data_ptr(), weights.packed.numel(), weights.n_adapters,
+                                 weights.rank, S.data_ptr(), row_begin, row_end,
+                                 adapter.data_ptr() if adapter is not None else None, Q.data_ptr(), K.data_ptr(),
+                                 V.data_ptr(), _stream())
+    _check(rc, where)
 
 
 def _store_call(where: str, cfg: LayerConfig, fmt: str, codes, scales, ids, rows, row_begin, row_end, n_store):

@@ -154,6 +154,17 @@ SweepEvents& sweep_events() { static SweepEvents e; return e; }
 // rows are read and written as 16-byte pieces
 template <typename... P> bool aligned16(P... ptrs) { return (((uintptr_t)ptrs | ...) & 15) == 0; }
 
+// What the calls with low-rank adapters share (no adapters: the rank is not looked at)
+int check_lora(const dg4_layer_cfg* cfg, int32_t n_adapters, int32_t* rank)
+{
+    const int rc = check_cfg(cfg, false);
+    if (rc != DG4_OK) return rc;
+    if (n_adapters < 0) return DG4_EINVAL;
+    if (n_adapters == 0) *rank = 1;
+    if (*rank < 1) return DG4_EINVAL;
+    return *rank > DG4_MAX_RANK ? DG4_EUNSUPPORTED : DG4_OK;
+}
+
 // What the calls on a K|V store in 8 bits share: configuration, the store's two arrays, the range of rows
 int check_kv8(const dg4_layer_cfg* cfg, int32_t format, const int32_t* ids, const uint8_t* codes, const uint8_t* scales,
               int64_t n_store, int64_t row_begin, int64_t row_end)
@@ -321,6 +332,57 @@ extern "C" int dg4_sparse_attn_fwd(const dg4_layer_cfg* cfg, dg4_graph* g, int64
     a.a = A; a.a_stride = d;
     a.row_begin = row_begin; a.row_end = row_end;
     HIPCHK(dg4_launch_attn(cfg->dtype, d, a, (hipStream_t)stream));
+    return DG4_OK;
+}
+
+extern "C" int64_t dg4_lora_packed_bytes(const dg4_layer_cfg* cfg, int32_t n_adapters, int32_t rank)
+{
+    const int rc = check_lora(cfg, n_adapters, &rank);
+    if (rc != DG4_OK) return rc;
+    int64_t down, up, gain;
+    return dg4_lora_bytes(cfg->dtype, cfg->hidden, n_adapters, rank, &down, &up, &gain);
+}
+
+extern "C" int dg4_lora_pack(const dg4_layer_cfg* cfg, const void* Wqkv, int32_t n_adapters, int32_t rank,
+                             const void* Down, const void* Up, const float* gain,
+                             void* packed, int64_t packed_bytes, void* stream)
+{
+    const int rc = check_lora(cfg, n_adapters, &rank);
+    if (rc != DG4_OK) return rc;
+    if (!Wqkv || !aligned16(Wqkv)) return DG4_EINVAL;
+    if (n_adapters > 0 && (!Down || !Up || !aligned16(Down, Up) || ((uintptr_t)gain & 3))) return DG4_EINVAL;
+    int64_t down_at, up_at, gain_at;
+    const int64_t need = dg4_lora_bytes(cfg->dtype, cfg->hidden, n_adapters, rank, &down_at, &up_at, &gain_at);
+    if (!packed || ((uintptr_t)packed & 255) || packed_bytes < need) return DG4_EWORKSPACE;
+    dg4_lora_pack_args a{};
+    a.w = Wqkv; a.down = Down; a.up = Up; a.gain = gain;
+    a.n_adapters = n_adapters; a.rank = rank;
+    char* base = (char*)packed;
+    a.w_packed = base; a.down_packed = base + down_at; a.up_packed = base + up_at; a.gain_packed = (float*)(base + gain_at);
+    HIPCHK(dg4_launch_lora_pack(cfg->dtype, cfg->hidden, a, (hipStream_t)stream));
+    return DG4_OK;
+}
+
+extern "C" int dg4_qkv_proj_lora(const dg4_layer_cfg* cfg, const void* packed, int64_t packed_bytes,
+                                 int32_t n_adapters, int32_t rank, const void* S, int64_t row_begin, int64_t row_end,
+                                 const int32_t* adapter, void* Q, void* K, void* V, void* stream)
+{
+    const int rc = check_lora(cfg, n_adapters, &rank);
+    if (rc != DG4_OK) return rc;
+    if (!S || !Q || !K || !V || row_begin < 0 || row_end < row_begin) return DG4_EINVAL;
+    if (!aligned16(S, Q, K, V) || ((uintptr_t)adapter & 3)) return DG4_EINVAL;
+    int64_t down_at, up_at, gain_at;
+    const int64_t need = dg4_lora_bytes(cfg->dtype, cfg->hidden, n_adapters, rank, &down_at, &up_at, &gain_at);
+    if (!packed || ((uintptr_t)packed & 255) || packed_bytes < need) return DG4_EWORKSPACE;
+    if (row_end == row_begin) return DG4_OK;
+    dg4_lora_args a{};
+    a.s = S; a.adapter = adapter;
+    a.n_adapters = n_adapters; a.rank = rank;
+    const char* base = (const char*)packed;
+    a.w_packed = base; a.down_packed = base + down_at; a.up_packed = base + up_at; a.gain_packed = (const float*)(base + gain_at);
+    a.out[0] = Q; a.out[1] = K; a.out[2] = V;
+    a.row_begin = row_begin; a.row_end = row_end;
+    HIPCHK(dg4_launch_lora_proj(cfg->dtype, cfg->hidden, a, (hipStream_t)stream));
     return DG4_OK;
 }
 

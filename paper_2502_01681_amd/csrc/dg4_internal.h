@@ -366,6 +366,28 @@ int dg4_launch_kv8_write(int dtype, int format, int hidden, const dg4_kv8_args& 
 int dg4_launch_kv8_read(int dtype, int format, int hidden, const dg4_kv8_args& a, hipStream_t s);
 int dg4_launch_kv8_attn(int dtype, int format, int hidden, const dg4_kv8_attn_args& a, hipStream_t s);
 
+// ---- Q|K|V projection with low-rank adapters (dg4_lora.hip) ----
+struct dg4_lora_pack_args {
+    const void* w;                         // [d, 3d]
+    const void* down; const void* up;      // [n_adapters, d, rank], [n_adapters, rank, 3d]
+    const float* gain;                     // nullable: [n_adapters], else 1
+    int64_t n_adapters; int rank; int rank8;                   // rank8: rounded up to eight (set by the launcher)
+    void* w_packed; void* down_packed; void* up_packed; float* gain_packed;
+};
+struct dg4_lora_args {
+    const void* s;                         // [*, d] rows
+    const int32_t* adapter;                // nullable: of every row; none if outside [0, n_adapters)
+    int64_t n_adapters; int rank; int rank8;
+    const void* w_packed; const void* down_packed; const void* up_packed; const float* gain_packed;
+    void* out[3];                          // Q, K, V [*, d] rows
+    int64_t row_begin, row_end;
+    int tile_rows;                         // rows of a tile in calls with few rows (set by the launcher)
+};
+// bytes of the packed weights, and where the parts behind W begin
+int64_t dg4_lora_bytes(int dtype, int hidden, int64_t n_adapters, int rank, int64_t* down, int64_t* up, int64_t* gain);
+int dg4_launch_lora_pack(int dtype, int hidden, dg4_lora_pack_args a, hipStream_t s);
+int dg4_launch_lora_proj(int dtype, int hidden, dg4_lora_args a, hipStream_t s);
+
 // Every kernel takes its argument block by value: plain data of pointer alignment, well inside the
 // kernel-argument segment (4 KB), value-initialised by every caller before the fields are set.
 #define DG4_CHECK_KERNEL_ARGS(S) \
@@ -379,5 +401,7 @@ DG4_CHECK_KERNEL_ARGS(dg4_bulk_args);
 DG4_CHECK_KERNEL_ARGS(dg4_heads_args);
 DG4_CHECK_KERNEL_ARGS(dg4_kv8_args);
 DG4_CHECK_KERNEL_ARGS(dg4_kv8_attn_args);
+DG4_CHECK_KERNEL_ARGS(dg4_lora_pack_args);
+DG4_CHECK_KERNEL_ARGS(dg4_lora_args);
 DG4_CHECK_KERNEL_ARGS(dg4_heads_pack_args);
 #undef DG4_CHECK_KERNEL_ARGS
