@@ -352,14 +352,25 @@ def dg4_sparse_attn_fwd(cfg: LayerConfig, g: Graph, Q, K, V, rel_bias, A, row_be
     _check(rc, "dg4_sparse_attn_fwd")
 
 
-def _tensors(where: str, *wanted):
-    """(tensor, element type, columns) each: contiguous rows on the current device, or EINVAL."""
-    import torch
-    dev = torch.cuda.current_device()
-    for t, dtype, cols in wanted:
-        if t.dtype != dtype or not t.is_cuda or t.get_device() != dev or not t.is_contiguous() or \
-           (cols is not None and (t.dim() < 2 or t.shape[0] and t.numel() // t.shape[0] != cols)):
-            raise DG4Error(-1, where)
+_types = None                    # element types of cfg.dtype, index and byte, once torch is there
+
+
+def _refused(t, dtype, dev, count) -> bool:
+    """Whether a tensor is anything but `count` contiguous elements of one type on the device."""
+    return t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous() or t.numel() != count
+
+
+def _call(where: str, cfg: LayerConfig, first):
+    """Element type of the configuration, the current device and its stream, for a call on `first`'s device."""
+    global _types, _raw_stream, _device
+    if _types is None:
+        import torch
+        _types = {"f32": torch.float32, "bf16": torch.bfloat16, "ids": torch.int32, "bytes": torch.uint8}
+        _raw_stream, _device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+    dev = first.get_device()
+    if cfg.dtype not in ("f32", "bf16") or dev < 0 or dev != _device():
+        raise DG4Error(-1, where)
+    return _types[cfg.dtype], dev, _raw_stream(dev)
 
 
 @dataclass
@@ -383,28 +394,20 @@ def dg4_lora_packed_bytes(cfg: LayerConfig, n_adapters: int, rank: int) -> int:
 def dg4_lora_pack(cfg: LayerConfig, Wqkv, Down=None, Up=None, gain=None) -> LoraWeights:
     """Wqkv [hidden, 3*hidden], Down [n_adapters, hidden, rank], Up [n_adapters, rank, 3*hidden], gain float [n_adapters]
     (None: 1); without Down and Up the projection alone."""
-    import torch
-    where = "dg4_lora_pack"
-    if cfg.dtype not in ("f32", "bf16") or (Down is None) != (Up is None):
+    where, d = "dg4_lora_pack", cfg.hidden
+    td, dev, stream = _call(where, cfg, Wqkv)
+    if (Down is None) != (Up is None):
         raise DG4Error(-1, where)
-    td = torch.float32 if cfg.dtype == "f32" else torch.bfloat16
-    _tensors(where, (Wqkv, td, 3 * cfg.hidden))
     n, rank = (0, 1) if Down is None else (Down.shape[0], Down.shape[-1])
-    if n:
-        _tensors(where, (Down, td, None), (Up, td, None))
-        if tuple(Down.shape) != (n, cfg.hidden, rank) or tuple(Up.shape) != (n, rank, 3 * cfg.hidden):
-            raise DG4Error(-1, where)
-        if gain is not None:
-            _tensors(where, (gain, torch.float32, None))
-            if gain.numel() != n:
-                raise DG4Error(-1, where)
-    if Wqkv.shape[0] != cfg.hidden:
+    if _refused(Wqkv, td, dev, 3 * d * d) or n and (
+            tuple(Down.shape) != (n, d, rank) or tuple(Up.shape) != (n, rank, 3 * d) or _refused(Down, td, dev, n * d * rank) or
+            _refused(Up, td, dev, 3 * n * d * rank) or gain is not None and _refused(gain, _types["f32"], dev, n)):
         raise DG4Error(-1, where)
     packed = _ws(dg4_lora_packed_bytes(cfg, n, rank), Wqkv)
     c = cfg.c()
     rc = lib().dg4_lora_pack(ctypes.byref(c), Wqkv.data_ptr(), n, rank, Down.data_ptr() if n else None,
                              Up.data_ptr() if n else None, gain.data_ptr() if n and gain is not None else None,
-                             packed.data_ptr(), packed.numel(), _stream())
+                             packed.data_ptr(), packed.numel(), stream)
     _check(rc, where)
     return LoraWeights(packed, n, rank, cfg.hidden, cfg.dtype)
 
@@ -412,75 +415,73 @@ def dg4_lora_pack(cfg: LayerConfig, Wqkv, Down=None, Up=None, gain=None) -> Lora
 def dg4_qkv_proj_lora(cfg: LayerConfig, weights: LoraWeights, S, adapter, Q, K, V, row_begin=0, row_end=None):
     """Q, K, V rows [row_begin,row_end) = S rows x Wqkv + what the adapter of each row adds (int32, one of every row of S;
     None or outside [0, n_adapters): nothing). In place."""
-    import torch
-    where = "dg4_qkv_proj_lora"
-    if cfg.dtype != weights.dtype or cfg.hidden != weights.hidden:
+    where, d, rows = "dg4_qkv_proj_lora", cfg.hidden, S.shape[0]
+    td, dev, stream = _call(where, cfg, S)
+    row_end = rows if row_end is None else row_end
+    if (cfg.dtype != weights.dtype or d != weights.hidden or row_end > rows or weights.packed.get_device() != dev or
+            _refused(S, td, dev, rows * d) or _refused(Q, td, dev, rows * d) or _refused(K, td, dev, rows * d) or
+            _refused(V, td, dev, rows * d) or adapter is not None and _refused(adapter, _types["ids"], dev, rows)):
         raise DG4Error(-1, where)
-    td = torch.float32 if cfg.dtype == "f32" else torch.bfloat16
-    _tensors(where, (S, td, cfg.hidden), (Q, td, cfg.hidden), (K, td, cfg.hidden), (V, td, cfg.hidden))
-    have = min(S.shape[0], Q.shape[0], K.shape[0], V.shape[0])
-    if adapter is not None:
-        _tensors(where, (adapter, torch.int32, None))
-        have = min(have, adapter.numel())
-    row_end = S.shape[0] if row_end is None else row_end
-    if row_end > have:
-        raise DG4Error(-1, where)
+    if row_begin == row_end == 0:                # (an empty tensor has no address)
+        return
+    packed = weights.packed
     c = cfg.c()
-    rc = lib().dg4_qkv_proj_lora(ctypes.byref(c), weights.packed.data_ptr(), weights.packed.numel(), weights.n_adapters,
-                                 weights.rank, S.data_ptr(), row_begin, row_end,
-                                 adapter.data_ptr() if adapter is not None else None, Q.data_ptr(), K.data_ptr(),
-                                 V.data_ptr(), _stream())
+    rc = lib().dg4_qkv_proj_lora(ctypes.byref(c), packed.data_ptr(), packed.numel(), weights.n_adapters, weights.rank,
+                                 S.data_ptr(), row_begin, row_end, adapter.data_ptr() if adapter is not None else None,
+                                 Q.data_ptr(), K.data_ptr(), V.data_ptr(), stream)
     _check(rc, where)
 
 
-def _store_call(where: str, cfg: LayerConfig, fmt: str, codes, scales, ids, rows, row_begin, row_end, n_store):
-    """What the calls on a K|V store in 8 bits check and fill in: (format, end of the range, store rows, ids)."""
-    import torch
-    if fmt not in KV_FORMATS or cfg.dtype not in ("f32", "bf16") or any(t.shape[0] != rows[0].shape[0] for t in rows):
+def _store_call(where: str, cfg: LayerConfig, fmt: str, codes, scales, ids, x, y, row_begin, row_end):
+    """What the calls on a K|V store in 8 bits check and fill in, for rows x and y beside it: (format or, with nothing to
+    do, None; end of the range; store rows; address of ids; stream)."""
+    td, dev, stream = _call(where, cfg, codes)
+    n, rows = codes.shape[0], x.shape[0]
+    row_end = rows if row_end is None else row_end
+    if (fmt not in KV_FORMATS or row_end > rows or _refused(x, td, dev, rows * cfg.hidden) or
+            _refused(y, td, dev, rows * cfg.hidden) or _refused(codes, _types["bytes"], dev, n * 2 * cfg.hidden) or
+            _refused(scales, _types["bytes"], dev, n * 2 * cfg.heads) or
+            ids is not None and _refused(ids, _types["ids"], dev, rows)):
         raise DG4Error(-1, where)
-    td = torch.float32 if cfg.dtype == "f32" else torch.bfloat16
-    _tensors(where, (codes, torch.uint8, 2 * cfg.hidden), (scales, torch.uint8, 2 * cfg.heads), *((t, td, cfg.hidden) for t in rows))
-    have = rows[0].shape[0]
-    if ids is not None:
-        _tensors(where, (ids, torch.int32, None))
-        have = min(have, ids.numel())
-    n_store = min(codes.shape[0], scales.shape[0]) if n_store is None else n_store
-    row_end = rows[0].shape[0] if row_end is None else row_end
-    if row_end > have or n_store > min(codes.shape[0], scales.shape[0]):
-        raise DG4Error(-1, where)
-    return KV_FORMATS[fmt], row_end, n_store, ids.data_ptr() if ids is not None else None
+    if row_begin == row_end == 0 or n == 0 and ids is not None:      # (an empty tensor has no address)
+        return None, 0, n, None, stream
+    return KV_FORMATS[fmt], row_end, n, ids.data_ptr() if ids is not None else None, stream
 
 
 def dg4_kv8_write(cfg: LayerConfig, fmt: str, K, V, codes, scales, ids=None, row_begin=0, row_end=None):
     """Rows [row_begin,row_end) of K and V into the 8-bit store (fmt "e4m3" | "int8"): codes uint8 [n, 2*hidden] and
     scales uint8 [n, heads, 2] in place. ids: int32 store row of each row (outside the store: skipped), else the row itself."""
-    f, row_end, n, ip = _store_call("dg4_kv8_write", cfg, fmt, codes, scales, ids, (K, V), row_begin, row_end, None)
+    f, row_end, n, ip, stream = _store_call("dg4_kv8_write", cfg, fmt, codes, scales, ids, K, V, row_begin, row_end)
+    if f is None:
+        return
     c = cfg.c()
     rc = lib().dg4_kv8_write(ctypes.byref(c), f, K.data_ptr(), V.data_ptr(), row_begin, row_end, ip, codes.data_ptr(),
-                             scales.data_ptr(), n, _stream())
+                             scales.data_ptr(), n, stream)
     _check(rc, "dg4_kv8_write")
 
 
 def dg4_kv8_read(cfg: LayerConfig, fmt: str, codes, scales, K, V, ids=None, row_begin=0, row_end=None):
     """Rows [row_begin,row_end) of K and V, in place, from the 8-bit store; ids as in dg4_kv8_write."""
-    f, row_end, n, ip = _store_call("dg4_kv8_read", cfg, fmt, codes, scales, ids, (K, V), row_begin, row_end, None)
+    f, row_end, n, ip, stream = _store_call("dg4_kv8_read", cfg, fmt, codes, scales, ids, K, V, row_begin, row_end)
+    if f is None:
+        return
     c = cfg.c()
     rc = lib().dg4_kv8_read(ctypes.byref(c), f, codes.data_ptr(), scales.data_ptr(), n, ip, row_begin, row_end,
-                            K.data_ptr(), V.data_ptr(), _stream())
+                            K.data_ptr(), V.data_ptr(), stream)
     _check(rc, "dg4_kv8_read")
 
 
 def dg4_sparse_attn_kv8_fwd(cfg: LayerConfig, fmt: str, g: Graph, Q, codes, scales, rel_bias, A, ids=None, row_begin=0,
                             row_end=None):
     """Cone attention over the 8-bit store (row = node id). ids: int32 gate of each row of Q and A, else the row itself."""
-    import torch
-    f, row_end, _, ip = _store_call("dg4_sparse_attn_kv8_fwd", cfg, fmt, codes, scales, ids, (Q, A), row_begin, row_end, g.n)
-    _tensors("dg4_sparse_attn_kv8_fwd", (rel_bias, torch.float32, 4))
-    if rel_bias.shape[0] != cfg.heads:
+    f, row_end, n, ip, stream = _store_call("dg4_sparse_attn_kv8_fwd", cfg, fmt, codes, scales, ids, Q, A, row_begin, row_end)
+    if n < g.n or _refused(rel_bias, _types["f32"], codes.get_device(), 4 * cfg.heads):
         raise DG4Error(-1, "dg4_sparse_attn_kv8_fwd")
+    if f is None:
+        return
     c = cfg.c()
     rc = lib().dg4_sparse_attn_kv8_fwd(ctypes.byref(c), f, g.handle, row_begin, row_end, ip, Q.data_ptr(), codes.data_ptr(),
-                                       scales.data_ptr(), rel_bias.data_ptr(), A.data_ptr(), _stream())
+                                       scales.data_ptr(), rel_bias.data_ptr(), A.data_ptr(), stream)
     _check(rc, "dg4_sparse_attn_kv8_fwd")
 
 

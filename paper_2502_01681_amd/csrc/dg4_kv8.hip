@@ -11,10 +11,24 @@
 
 #include "dg4_device.h"
 #include "dg4_internal.h"
+#include "dg4_rowops.h"
 
 namespace {
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+// Bytes of codes up to which buffer addressing is used: offsets are 32 bits, and there is room for one that is past the end
+constexpr uint32_t KV8_NEAR_BYTES = 0xC0000000u;
+
+// Which run of rows a workgroup takes. Workgroups go to the eight XCDs in turn, and neighbouring rows read the same sources:
+// runs of 128 workgroups (1024 to 4096 rows) go to one XCD, so that its L2 serves them (a million gates of bf16 / 256, two
+// hops: lines missed in the L2s 30 M -> 18 M, 491 -> 452 us). What is left behind the last eight whole runs goes in turn.
+__device__ __forceinline__ uint32_t kv8_block(uint32_t block, uint32_t blocks)
+{
+    constexpr uint32_t RUN = 128;
+    const uint32_t base = block / (8 * RUN) * (8 * RUN);
+    return base + 8 * RUN <= blocks ? base + block % 8 * RUN + (block - base) / 8 : block;
+}
 
 // What a block is scaled by, from the bits of its largest magnitude: the biased exponent of the smallest power of two with
 // which that magnitude stays within the format's largest code, 448 = 1.75 * 2^8 or 127 = 1.984375 * 2^6. Adding what the
@@ -59,11 +73,6 @@ template <int FMT> __device__ __forceinline__ void decode4(uint32_t w, float* f)
         for (int i = 0; i < 4; ++i) f[i] = (float)(int8_t)(w >> (8 * i));
     }
 }
-template <int FMT> __device__ __forceinline__ void decode16(const uint4& w, float* f)
-{
-    decode4<FMT>(w.x, f); decode4<FMT>(w.y, f + 4); decode4<FMT>(w.z, f + 8); decode4<FMT>(w.w, f + 12);
-}
-
 // Eight values of a row in one lane, as loaded
 template <typename T> struct Eight;
 template <> struct Eight<float> {
@@ -170,147 +179,225 @@ __global__ __launch_bounds__(256) void kv8_read_kernel(dg4_kv8_args p)
 
 // ------------------------------------------------------------------------------------------------- attention
 
-// One destination row per S groups of D / 16 lanes; a lane owns 16 features (half a head). Chunks of CH entries go to the
-// groups in turn, each keeps a running maximum, denominator and weighted sum (32 bits), and the groups' results are joined
-// at the end: by lane exchange inside a wave, through LDS where WPR waves share the row. Entries that are none (padding, a
-// relation whose bias is -inf) are not read, so what the store holds there cannot matter.
-template <typename T, int FMT, int D, int S, int WPR, int CH>
+// Results leave past the caches, which are the store's (1 to 7 % of the time)
+__device__ __forceinline__ void store_stream(void* p, const uint4& v)
+{
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), (u32x4*)p);
+}
+
+// What an entry that is none reads where buffer addressing does not reach (FAR, below)
+__device__ __align__(256) const uint8_t nothing[512] = {};
+
+__device__ dg4_i32x4 dg4_raw_buffer_load16(dg4_i32x4 rsrc, int voffset, int soffset, int aux) __asm("llvm.amdgcn.raw.buffer.load.v4i32");
+__device__ uint16_t dg4_raw_buffer_load2(dg4_i32x4 rsrc, int voffset, int soffset, int aux) __asm("llvm.amdgcn.raw.buffer.load.i16");
+
+// The four codes of a word. e4m3: times the power of two of `byte`, which the conversion takes along (0: 2^-127, 255: NaN);
+// int8: as they are.
+template <int FMT> __device__ __forceinline__ void decode4_scaled(uint32_t w, uint32_t byte, float* f)
+{
+    if constexpr (FMT == DG4_KV_E4M3) {
+        const float scale = __uint_as_float(byte << 23);
+        const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, scale, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, scale, true);
+        f[0] = lo.x; f[1] = lo.y; f[2] = hi.x; f[3] = hi.y;
+    } else {
+        decode4<FMT>(w, f);
+    }
+}
+
+// A lane's sixteen values of q, and their product with as many codes (without the scale in int8). bfloat16 against e4m3:
+// pairs of bfloat16 numbers, which hold a code times its power of two exactly, two products and a sum in fp32 per instruction.
+template <typename T, int FMT> struct LaneQ {
+    float q[16];
+    __device__ __forceinline__ void load(const T* p)
+    {
+        const uint4* v = (const uint4*)p;
+        if constexpr (sizeof(T) == 2) {
+            Elem<bf16_t>::unpack(v[0], v[1], q);
+        } else {
+            Elem<float>::unpack(v[0], v[1], q);
+            Elem<float>::unpack(v[2], v[3], q + 8);
+        }
+    }
+    __device__ __forceinline__ float dot(const uint4& w, uint32_t byte) const
+    {
+        const uint32_t words[4] = { w.x, w.y, w.z, w.w };
+        float d = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float k[4];
+            decode4_scaled<FMT>(words[i], byte, k);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) d = i + x == 0 ? q[0] * k[0] : fmaf(q[4 * i + x], k[x], d);
+        }
+        return d;
+    }
+};
+template <> struct LaneQ<bf16_t, DG4_KV_E4M3> {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    uint4 a, b;
+    __device__ __forceinline__ void load(const bf16_t* p) { a = ((const uint4*)p)[0]; b = ((const uint4*)p)[1]; }
+    __device__ __forceinline__ float dot(const uint4& w, uint32_t byte) const
+    {
+        const float scale = __uint_as_float(byte << 23);
+        float d = 0.f;
+        auto four = [&](uint32_t codes, uint32_t q0, uint32_t q1) __attribute__((always_inline)) {
+            d = __builtin_amdgcn_fdot2_f32_bf16(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, false), __builtin_bit_cast(bf16x2, q0), d, false);
+            d = __builtin_amdgcn_fdot2_f32_bf16(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, true), __builtin_bit_cast(bf16x2, q1), d, false);
+        };
+        four(w.x, a.x, a.y); four(w.y, a.z, a.w); four(w.z, b.x, b.y); four(w.w, b.z, b.w);
+        return d;
+    }
+};
+
+// A lane owns sixteen features (half a head) and a destination row is S groups of D / 16 lanes: a source's K codes are one
+// load instruction over whole 128-byte lines, its V codes another. The row's entries go to the groups in turn, CH at a time;
+// each group keeps a running maximum, denominator and weighted sum (32 bits), joined at the end by lane exchange. ONCE: the
+// groups take the whole row at one go. Entries that are none (padding, a relation whose bias is -inf) ask the buffers for an
+// offset past the end: zeros, no request, no branch, and what the store holds there cannot matter. The offsets of buffer
+// addressing are 32 bits: FAR, for larger stores, has addresses of 64 bits and reads zeros from memory for them.
+template <typename T, int FMT, int D, int S, int CH, bool ONCE, bool FAR>
 __global__ __launch_bounds__(256) void kv8_attn_kernel(dg4_kv8_attn_args p)
 {
-    constexpr int LPR = D / 16, GPW = 64 / LPR;
+    constexpr int LPR = D / 16, HEADS = D / 32, GPW = 64 / LPR;
     constexpr int RPW = GPW / S;                  // rows per wave
-    static_assert(WPR == 1 || (S == GPW && WPR == 4), "a row is a part of a wave, a wave or the workgroup");
-    constexpr int PARTS = S * WPR;
+    constexpr uint32_t NONE = KV8_NEAR_BYTES / (2 * D);        // past the end of a store that buffer addressing reaches
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int sub = lane % LPR, group = lane / LPR;
-    const int part = WPR == 1 ? group % S : wave * S + group;
-    const int64_t r = WPR == 1 ? p.row_begin + ((int64_t)blockIdx.x * 4 + wave) * RPW + group / S : p.row_begin + blockIdx.x;
+    const int sub = lane % LPR, group = lane / LPR, part = group % S;
+    const int head = sub >> 1;
+    // biases of a head by relation code
+    __shared__ float bias[HEADS][4];
+    if (threadIdx.x < HEADS * 4) bias[threadIdx.x / 4][threadIdx.x % 4] = p.rel_bias[threadIdx.x];
+    __syncthreads();
+    const int64_t r = p.row_begin + ((int64_t)(ONCE ? kv8_block(blockIdx.x, gridDim.x) : blockIdx.x) * 4 + wave) * RPW + group / S;
     // (what leaves here leaves as whole rows)
     if (r >= p.row_end) return;
     const int64_t v = p.ids ? (int64_t)p.ids[r] : r;
     if (v < 0 || v >= p.n) return;
-    const int head = sub >> 1;
 
-    const uint8_t* codes = p.codes + sub * 16;
-    const uint8_t* scales = p.scales + head * 2;
+    const dg4_i32x4 code_bytes = row_buffer(p.codes, 0, FAR ? 0 : (uint32_t)(p.n * 2 * D));
+    const dg4_i32x4 scale_bytes = row_buffer(p.scales, 0, FAR ? 0 : (uint32_t)(p.n * 2 * HEADS));
     const uint32_t* erow = p.ell + v * (int64_t)p.ell_w;
-    auto entries = [&](int c0, uint32_t (&e)[CH]) __attribute__((always_inline)) {
+    uint4 ent[CH / 4];
+    auto entries = [&](int c0) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < CH; i += 4) {
-            const uint4 e4 = c0 + i < p.ell_w ? *(const uint4*)(erow + c0 + i) : make_uint4(DG4_ELL_PAD, DG4_ELL_PAD, DG4_ELL_PAD, DG4_ELL_PAD);
-            e[i] = e4.x; e[i + 1] = e4.y; e[i + 2] = e4.z; e[i + 3] = e4.w;
-        }
+        for (int i = 0; i < CH / 4; ++i)
+            ent[i] = c0 + 4 * i < p.ell_w ? *(const uint4*)(erow + c0 + 4 * i) : make_uint4(DG4_ELL_PAD, DG4_ELL_PAD, DG4_ELL_PAD, DG4_ELL_PAD);
     };
-    uint32_t ent[CH];
-    entries(part * CH, ent);
-    const float* bp = p.rel_bias + head * 4;
-    const float4 bias = make_float4(bp[0], bp[1], bp[2], bp[3]);
-    float q[16];
-    {
-        const uint4* qp = (const uint4*)((const T*)p.q + r * D + sub * 16);
-        if constexpr (sizeof(T) == 2) {
-            Elem<bf16_t>::unpack(qp[0], qp[1], q);
-        } else {
-            Elem<float>::unpack(qp[0], qp[1], q);
-            Elem<float>::unpack(qp[2], qp[3], q + 8);
-        }
-    }
+    entries(part * CH);
+    LaneQ<T, FMT> q;
+    q.load((const T*)p.q + r * D + sub * 16);
     const float c = 0.17677669529663687f;         // 1/sqrt(32)
     const float log2e = 1.4426950408889634f;
     float m = -INFINITY, z = 0.f;
     float acc[16];
+    if constexpr (!ONCE) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) acc[i] = 0.f;
-
-    for (int c0 = part * CH; c0 < p.ell_w; c0 += PARTS * CH) {
-        if (ent[0] == DG4_ELL_PAD) break;         // padding stands at the end only; the same for all lanes of the group
+        for (int i = 0; i < 16; ++i) acc[i] = 0.f;
+    }
+    for (int c0 = part * CH; ONCE || c0 < p.ell_w; c0 += S * CH) {
+        if (!ONCE && ent[0].x == DG4_ELL_PAD) break;           // padding stands at the end only; the same for all lanes of the group
         uint4 kw[CH], vw[CH];
-        uint32_t sw[CH];
+        uint32_t sw[CH];                          // scales: of K, and of V from bit 8
         float b[CH];
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
-            const uint32_t rel = ent[j] >> 30;
-            b[j] = ent[j] == DG4_ELL_PAD ? -INFINITY : rel == 0 ? bias.x : rel == 1 ? bias.y : rel == 2 ? bias.z : bias.w;
-            if (b[j] != -INFINITY) {
-                const int64_t row = ent[j] & 0x3FFFFFFFu;
-                sw[j] = *(const uint16_t*)(scales + row * (2 * D / 32));
-                kw[j] = *(const uint4*)(codes + row * (2 * D));
-                vw[j] = *(const uint4*)(codes + row * (2 * D) + D);
+            const uint32_t e = j % 4 == 0 ? ent[j / 4].x : j % 4 == 1 ? ent[j / 4].y : j % 4 == 2 ? ent[j / 4].z : ent[j / 4].w;
+            const float bj = bias[head][e >> 30];
+            b[j] = e == DG4_ELL_PAD ? -INFINITY : bj;
+            const bool none = b[j] == -INFINITY;
+            if constexpr (FAR) {
+                const int64_t row = e & 0x3FFFFFFFu;
+                const uint8_t* at = none ? nothing : p.codes + row * (2 * D);
+                sw[j] = *(const uint16_t*)((none ? nothing : p.scales + row * (2 * HEADS)) + head * 2);
+                kw[j] = *(const uint4*)(at + sub * 16);
+                vw[j] = *(const uint4*)(at + D + sub * 16);
             } else {
-                sw[j] = 0;
-                kw[j] = make_uint4(0, 0, 0, 0); vw[j] = kw[j];
+                const uint32_t row = none ? NONE : e & 0x3FFFFFFFu;
+                const int at = (int)(row * (2 * D) + sub * 16);
+                sw[j] = dg4_raw_buffer_load2(scale_bytes, (int)(row * (2 * HEADS) + head * 2), 0, 0);
+                kw[j] = __builtin_bit_cast(uint4, dg4_raw_buffer_load16(code_bytes, at, 0, 0));
+                vw[j] = __builtin_bit_cast(uint4, dg4_raw_buffer_load16(code_bytes, at + D, 0, 0));
             }
         }
-        entries(c0 + PARTS * CH, ent);            // the next step's entries travel with this step's rows
+        if constexpr (!ONCE) entries(c0 + S * CH);             // the next step's entries travel with this step's rows
         float s[CH];
         float cm = m;
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
-            float k[16];
-            decode16<FMT>(kw[j], k);
-            float dot = 0.f;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) dot = fmaf(q[i], k[i], dot);
+            float dot = q.dot(kw[j], sw[j] & 255u);
             dot += xor1(dot);
-            s[j] = b[j] == -INFINITY ? -INFINITY : fmaf(dot, scale_value(sw[j] & 255u) * c, b[j]);
+            s[j] = fmaf(dot, FMT == DG4_KV_E4M3 ? c : scale_value(sw[j] & 255u) * c, b[j]);
             cm = fmaxf(cm, s[j]);
         }
         // (nothing so far: any finite base will do, every weight is 0)
         const float base = cm == -INFINITY ? 0.f : cm;
-        const float corr = __builtin_amdgcn_exp2f((m - base) * log2e);
-        z *= corr;
+        if constexpr (!ONCE) {
+            const float corr = __builtin_amdgcn_exp2f((m - base) * log2e);
+            z *= corr;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) acc[i] *= corr;
+            for (int i = 0; i < 16; ++i) acc[i] *= corr;
+        }
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
             const float pj = __builtin_amdgcn_exp2f((s[j] - base) * log2e);
             z += pj;
-            const float pv = pj * scale_value(sw[j] >> 8);
-            float x[16];
-            decode16<FMT>(vw[j], x);
+            const float pv = FMT == DG4_KV_E4M3 ? pj : pj * scale_value(sw[j] >> 8);
+            const uint32_t words[4] = { vw[j].x, vw[j].y, vw[j].z, vw[j].w };
 #pragma unroll
-            for (int i = 0; i < 16; ++i) acc[i] = fmaf(pv, x[i], acc[i]);
+            for (int i = 0; i < 4; ++i) {
+                float x[4];
+                decode4_scaled<FMT>(words[i], sw[j] >> 8, x);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) acc[4 * i + k] = ONCE && j == 0 ? pv * x[k] : fmaf(pv, x[k], acc[4 * i + k]);
+            }
         }
         m = cm;
+        if constexpr (ONCE) break;
     }
-    // join the groups of the row
-    auto join = [&](float m2, float z2, auto&& other) __attribute__((always_inline)) {
-        const float mm = fmaxf(m, m2), base = mm == -INFINITY ? 0.f : mm;
-        const float a = __builtin_amdgcn_exp2f((m - base) * log2e), b = __builtin_amdgcn_exp2f((m2 - base) * log2e);
-        z = z * a + z2 * b;
+    // join the groups of the row: one maximum, then sums, each exchange leaving a lane half the features it had
+    constexpr int KEPT = 16 / S;
+    int first = 0;
+    if constexpr (S > 1) {
+        float mm = m;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) acc[i] = acc[i] * a + other(i) * b;
-        m = mm;
-    };
+        for (int x = 1; x < S; x *= 2) mm = fmaxf(mm, __shfl_xor(mm, x * LPR));
+        const float f = __builtin_amdgcn_exp2f((m - (mm == -INFINITY ? 0.f : mm)) * log2e);
+        z *= f;
 #pragma unroll
-    for (int x = 1; x < S; x *= 2) join(__shfl_xor(m, x * LPR), __shfl_xor(z, x * LPR), [&](int i) { return __shfl_xor(acc[i], x * LPR); });
-    if constexpr (WPR > 1) {
-        __shared__ float sm[WPR][LPR], sz[WPR][LPR], sacc[WPR][16][LPR];
-        if (group == 0) {
-            sm[wave][sub] = m; sz[wave][sub] = z;
+        for (int i = 0; i < 16; ++i) acc[i] *= f;
+        auto halve = [&](auto distance) __attribute__((always_inline)) {
+            constexpr int x = distance, half = 16 * x / S;                 // features a lane keeps
+            const bool upper = (group & x) != 0;
+            z += __shfl_xor(z, x * LPR);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sacc[wave][i][sub] = acc[i];
-        }
-        __syncthreads();
-        if (wave != 0) return;
-#pragma unroll
-        for (int w = 1; w < WPR; ++w) join(sm[w][sub], sz[w][sub], [&](int i) { return sacc[w][i][sub]; });
+            for (int i = 0; i < half; ++i) {
+                const float keep = upper ? acc[i + half] : acc[i], give = upper ? acc[i] : acc[i + half];
+                acc[i] = keep + __shfl_xor(give, x * LPR);
+            }
+            first += upper ? half : 0;
+        };
+        static_assert(S <= 8 && KEPT % 2 == 0, "exchanges");
+        if constexpr (S >= 8) halve(std::integral_constant<int, 4>{});
+        if constexpr (S >= 4) halve(std::integral_constant<int, 2>{});
+        halve(std::integral_constant<int, 1>{});
     }
-    if (group % S != 0) return;
     const float rz = z == 0.f ? 0.f : 1.0f / z;
+    T* out = (T*)p.a + r * D + sub * 16 + first;
+    constexpr int WORDS = KEPT * (int)sizeof(T) / 4;
+    uint32_t w[WORDS];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) acc[i] *= rz;
-    uint4* op = (uint4*)((T*)p.a + r * D + sub * 16);
-    if constexpr (sizeof(T) == 2) {
-        uint4 oa, ob;
-        Elem<bf16_t>::pack(acc, oa, ob);
-        op[0] = oa; op[1] = ob;
+    for (int i = 0; i < KEPT; i += 2) {
+        if constexpr (sizeof(T) == 2) w[i / 2] = pack_bf16x2(acc[i] * rz, acc[i + 1] * rz);
+        else { w[i] = __float_as_uint(acc[i] * rz); w[i + 1] = __float_as_uint(acc[i + 1] * rz); }
+    }
+    if constexpr (WORDS >= 4) {
+#pragma unroll
+        for (int i = 0; i < WORDS; i += 4) store_stream(out + i * (4 / (int)sizeof(T)), make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]));
+    } else if constexpr (WORDS == 2) {
+        *(uint2*)out = make_uint2(w[0], w[1]);
     } else {
-        uint4 oa, ob;
-        Elem<float>::pack(acc, oa, ob);
-        op[0] = oa; op[1] = ob;
-        Elem<float>::pack(acc + 8, oa, ob);
-        op[2] = oa; op[3] = ob;
+        *(uint32_t*)out = w[0];
     }
 }
 
@@ -333,21 +420,24 @@ int launch_read(const dg4_kv8_args& a, hipStream_t s)
     return hipGetLastError();
 }
 // The split goes by the table's width alone, so a row's result does not depend on which rows a call covers.
-template <typename T, int FMT, int D>
-int launch_attn(const dg4_kv8_attn_args& a, hipStream_t s)
+template <typename T, int FMT, int D, bool FAR>
+int launch_attn_from(const dg4_kv8_attn_args& a, hipStream_t s)
 {
     constexpr int GPW = 64 / (D / 16);
     const int64_t rows = a.row_end - a.row_begin;
     auto grid = [&](int rows_per_block) { return dim3((unsigned)((rows + rows_per_block - 1) / rows_per_block)); };
     if (a.ell_w <= 8)
-        hipLaunchKernelGGL((kv8_attn_kernel<T, FMT, D, 1, 1, 8>), grid(4 * GPW), dim3(256), 0, s, a);
+        hipLaunchKernelGGL((kv8_attn_kernel<T, FMT, D, 2, 4, true, FAR>), grid(4 * GPW / 2), dim3(256), 0, s, a);
     else if (a.ell_w <= 16)
-        hipLaunchKernelGGL((kv8_attn_kernel<T, FMT, D, 2, 1, 8>), grid(4 * GPW / 2), dim3(256), 0, s, a);
-    else if (a.ell_w <= 64)
-        hipLaunchKernelGGL((kv8_attn_kernel<T, FMT, D, GPW, 1, 8>), grid(4), dim3(256), 0, s, a);
+        hipLaunchKernelGGL((kv8_attn_kernel<T, FMT, D, 2, 8, true, FAR>), grid(4 * GPW / 2), dim3(256), 0, s, a);
     else
-        hipLaunchKernelGGL((kv8_attn_kernel<T, FMT, D, GPW, 4, 8>), grid(1), dim3(256), 0, s, a);
+        hipLaunchKernelGGL((kv8_attn_kernel<T, FMT, D, GPW, 4, false, FAR>), grid(4), dim3(256), 0, s, a);
     return hipGetLastError();
+}
+template <typename T, int FMT, int D>
+int launch_attn(const dg4_kv8_attn_args& a, hipStream_t s)
+{
+    return a.n * (2 * D) <= (int64_t)KV8_NEAR_BYTES ? launch_attn_from<T, FMT, D, false>(a, s) : launch_attn_from<T, FMT, D, true>(a, s);
 }
 
 // f<T, format, hidden>() of the call's configuration

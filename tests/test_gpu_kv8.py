@@ -257,6 +257,40 @@ def test_relations_left_out(fmt, hops):
     assert (err <= bound).all(), (err / bound).max()
 
 
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("hops", [2, 5])
+def test_any_scale_and_code(fmt, dtype, hops):
+    """Stores as a caller may fill them: every code that is a number, scales from the smallest on."""
+    n, hidden = 90, 128
+    g = circuit(n, 30, hops, seed=4)
+    rng = np.random.default_rng(8)
+    codes = rng.integers(0, 256, (n, 2 * hidden)).astype(np.uint8)
+    if fmt == "e4m3":
+        codes[(codes & 127) == 127] = 0x7E
+    scales = rng.integers(105, 121, (n, 4, 2))
+    scales[rng.random(scales.shape) < 0.2] = 0
+    scales[rng.random(scales.shape) < 0.1] = 1
+    scales[:, :, 1] += rng.integers(0, 3, (n, 4)) * 30         # (values far apart in size)
+    codes, scales = torch.from_numpy(codes).cuda(), torch.from_numpy(scales.astype(np.uint8)).cuda()
+    Q = torch.from_numpy(rng.standard_normal((n, hidden)).astype(np.float32)).to(tdtype(dtype)).cuda()
+    bias = torch.from_numpy(rng.standard_normal((4, 4)).astype(np.float32)).cuda()
+    want, bound = reference(g, range(n), Q, codes, scales, fmt, bias, dtype)
+    A = torch.full_like(Q, 7.0)
+    dg4.dg4_sparse_attn_kv8_fwd(cfg(hidden, dtype, hops), fmt, g, Q, codes, scales, bias, A)
+    err = np.abs(to_np(A) - want)
+    assert (err <= bound).all(), (err / bound).max()
+    # a scale of 255 is NaN, whatever the codes
+    g1 = dg4.dg4_build_levels(4, [0, 1, 2], [2, 2, 3], [0, 0, 0], 1)
+    codes, scales = codes[:4].contiguous(), torch.full((4, 4, 2), 120, dtype=torch.uint8, device="cuda")
+    codes[0], codes[1] = 0, 1
+    scales[0, 1, 0] = scales[1, 2, 1] = 255
+    A = torch.zeros((4, hidden), dtype=Q.dtype, device="cuda")
+    dg4.dg4_sparse_attn_kv8_fwd(cfg(hidden, dtype, 1), fmt, g1, Q[:4].contiguous(), codes, scales, bias, A)
+    nan = A.isnan().view(4, 4, 32)
+    assert nan[0, 1].all() and nan[1, 2].all() and nan[2, 1].all() and nan[2, 2].all() and int(nan.sum()) == 4 * 32
+
+
 def test_what_is_left_out_may_hold_anything():
     n, hidden = 40, 256
     src, dst = [0, 1, 2, 3], [10, 10, 11, 11]
@@ -320,3 +354,53 @@ def test_captured_and_on_other_streams(hidden, dtype):
         calls()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, out + [codes, scales])), step
+
+
+def test_binding_checks():
+    """Shapes, types, formats and places that do not fit are turned away before anything is queued; nothing to do is fine."""
+    n, hidden = 6, 128
+    c = cfg(hidden, "f32")
+    g = dg4.dg4_build_levels(n, [0, 1], [2, 2], [0, 1], 2)
+    f = lambda *shape: torch.zeros(shape, device="cuda")
+    b = lambda *shape: torch.zeros(shape, dtype=torch.uint8, device="cuda")
+    i = lambda k, t=torch.int32: torch.zeros(k, dtype=t, device="cuda")
+    good = dict(x=f(n, hidden), y=f(n, hidden), codes=b(n, 256), scales=b(n, 4, 2), ids=i(n), fmt="int8", cfg=c, bias=f(4, 4))
+    bad = [dict(x=f(n, hidden).double()), dict(x=f(n, hidden).cpu()), dict(y=f(n - 1, hidden)), dict(x=f(hidden, n).t()), dict(codes=b(n, 255)),
+           dict(codes=b(n, 256).float()), dict(scales=b(n, 8, 2)), dict(scales=b(n - 1, 4, 2)), dict(ids=i(n - 1)), dict(ids=i(n, torch.int64)),
+           dict(ids=i(n).cpu()), dict(fmt="fp8"), dict(cfg=cfg(hidden, "bf16")), dict(cfg=dg4.LayerConfig(256, 8, 2, 1, "f32")),
+           dict(cfg=dg4.LayerConfig(hidden, 4, 2, 1, "f16")), dict(y=f(2 * n, hidden)[::2])]
+    attn_only = [dict(bias=f(3, 4)), dict(bias=f(4, 4).double()), dict(cfg=cfg(hidden, "f32", 3))]
+
+    def calls(x, y, codes, scales, ids, fmt, cfg, bias, **kw):
+        yield lambda: dg4.dg4_sparse_attn_kv8_fwd(cfg, fmt, g, x, codes, scales, bias, y, ids=ids, **kw)
+        yield lambda: dg4.dg4_kv8_write(cfg, fmt, x, y, codes, scales, ids=ids, **kw)
+        yield lambda: dg4.dg4_kv8_read(cfg, fmt, codes, scales, x, y, ids=ids, **kw)
+    for change in bad:
+        for call in calls(**{**good, **change}):
+            with pytest.raises(dg4.DG4Error):
+                call()
+    for change in attn_only:
+        with pytest.raises(dg4.DG4Error):
+            next(calls(**{**good, **change}))()
+    for rng in (dict(row_begin=-1), dict(row_end=n + 1), dict(row_begin=3, row_end=2)):
+        for call in calls(**good, **rng):
+            with pytest.raises(dg4.DG4Error):
+                call()
+    with pytest.raises(dg4.DG4Error):              # a store with fewer rows than the graph has gates
+        next(calls(**{**good, "codes": b(n - 1, 256), "scales": b(n - 1, 4, 2)}))()
+    empty = dict(good, x=f(0, hidden), y=f(0, hidden), ids=i(0))
+    for call in calls(**empty):
+        call()
+    for call in list(calls(**{**empty, "ids": None})) + list(calls(**good, row_begin=4, row_end=4)):
+        call()
+    none = dict(good, codes=b(0, 256), scales=b(0, 4, 2))
+    for call in list(calls(**none))[1:]:
+        call()
+    with pytest.raises(dg4.DG4Error):
+        list(calls(**{**none, "ids": None}))[1]()
+    torch.cuda.synchronize()
+    # rows given head by head are the same rows
+    a, z = f(n, 4, 32).normal_(), f(n, 4, 32)
+    dg4.dg4_kv8_write(c, "int8", a, a, good["codes"], good["scales"])
+    dg4.dg4_kv8_read(c, "int8", good["codes"], good["scales"], z, z.clone())
+    assert float((z - a).abs().max()) < 0.05

@@ -232,3 +232,28 @@ def test_two_graphs_and_a_stream_share_the_packed_weights():
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for got, w in zip(outs, want) for x, y in zip(got, w))
         assert all(torch.equal(x, y) for x, y in zip(eager, want[0]))
+
+
+def test_binding_checks():
+    d, n, rank, rows = 128, 3, 8, 10
+    cfg = dg4.LayerConfig(d, 4, 2, 1, "bf16")
+    W, down, up, gain = weights(1, d, n, rank, "bf16")
+    for args in ((W[:, :300], down, up, gain), (W.float(), down, up, gain), (W, down, None, gain), (W, down, up[:2], gain), (W, down.float(), up, gain),
+                 (W, down, up, gain[:2]), (W, down, up, gain.double()), (W, down.cpu(), up, gain), (W, down.transpose(1, 2), up, gain),
+                 (W.t(), down, up, gain), (W, torch.zeros((n, d, 65), dtype=W.dtype, device="cuda"), torch.zeros((n, 65, 3 * d), dtype=W.dtype, device="cuda"), gain)):
+        with pytest.raises(dg4.DG4Error):
+            dg4.dg4_lora_pack(cfg, *args)
+    packed = dg4.dg4_lora_pack(cfg, W, down, up, gain)
+    S, ad = rows_of(1, rows, d, "bf16"), torch.zeros(rows, dtype=torch.int32, device="cuda")
+    out = [torch.full_like(S, 7.0) for _ in range(3)]
+    for args, kw in (((S.float(), ad, *out), {}), ((S, ad.long(), *out), {}), ((S, ad[:9], *out), {}), ((S, ad, out[0][:9], *out[1:]), {}),
+                     ((S, ad, *out), dict(row_end=11)), ((S, ad, *out), dict(row_begin=-1)), ((S, ad, *out), dict(row_begin=5, row_end=4)),
+                     ((S.cpu(), ad, *out), {}), ((S, ad.cpu(), *out), {})):
+        with pytest.raises(dg4.DG4Error):
+            dg4.dg4_qkv_proj_lora(cfg, packed, *args, **kw)
+    with pytest.raises(dg4.DG4Error):
+        dg4.dg4_qkv_proj_lora(dg4.LayerConfig(d, 4, 2, 1, "f32"), packed, S.float(), ad, *(t.float() for t in out))
+    dg4.dg4_qkv_proj_lora(cfg, packed, S[:0], ad[:0], *(t[:0] for t in out))
+    dg4.dg4_qkv_proj_lora(cfg, packed, S, ad, *out, row_begin=6, row_end=6)
+    torch.cuda.synchronize()
+    assert all((t == 7.0).all() for t in out)

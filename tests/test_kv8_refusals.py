@@ -69,3 +69,15 @@ def test_reference_quantiser():
     x[0, 1] = np.inf
     assert ref.quantise(x, "int8")[1][0, 0] == 255
     assert ref.VALUES["e4m3"][0x7E] == 448.0 and ref.VALUES["e4m3"][1] == 2.0 ** -9 and ref.VALUES["int8"][0x80] == -128
+
+
+def test_binding_turns_away_what_is_not_on_the_device():
+    import torch
+    cfg = dg4.LayerConfig(128, 4, 2, 1, "f32")
+    x, codes, scales = torch.zeros((3, 128)), torch.zeros((3, 256), dtype=torch.uint8), torch.zeros((3, 4, 2), dtype=torch.uint8)
+    g = dg4.dg4_build_levels(3, [0, 1], [2, 2], [0, 1], 2)
+    for call in (lambda: dg4.dg4_kv8_write(cfg, "e4m3", x, x, codes, scales), lambda: dg4.dg4_kv8_read(cfg, "e4m3", codes, scales, x, x),
+                 lambda: dg4.dg4_sparse_attn_kv8_fwd(cfg, "e4m3", g, x, codes, scales, torch.zeros((4, 4)), x),
+                 lambda: dg4.dg4_lora_pack(cfg, torch.zeros((128, 384)))):
+        with pytest.raises(dg4.DG4Error):
+            call()
