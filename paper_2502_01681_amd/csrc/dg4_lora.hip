@@ -1,14 +1,17 @@
 // The Q|K|V projection with low-rank adapters: [Q|K|V][r] = S[r] W + gain_a (S[r] D_a) U_a with a = adapter[r], for rows of
 // many circuits at once, each with its own adapter or none.
 //
-//  lora_pack_kernel  lays W, D_a and U_a out once in matrix-core operand order.
-//  lora_proj_kernel  one launch: a tile of rows goes to LDS, T = gain (S D_a) for every row by its own adapter, then the
-//                    output columns, first T U_a, then S W on top in the same accumulators.
+//  lora_pack_kernel      lays W, D_a and U_a out once in matrix-core operand order.
+//  lora_stream_kernel    a tile of 32 rows goes to LDS, T = gain (S D_a) for every row by its own adapter, then the output
+//                        columns, first T U_a, then S W on top in the same accumulators, W streaming from the L2: fp32, and
+//                        calls with few rows.
+//  lora_resident_kernel  the same with W in registers and a workgroup walking over tiles of 64 rows, half of its waves
+//                        fetching rows and forming T ahead of the others: bfloat16, many rows.
 //
-// A row's arithmetic is the same whatever else its tile holds and however many rows a call covers: the products of a row on
-// the matrix cores do not see the other rows, T is always summed as two halves of the features, and where rows of a tile
-// differ in their adapter each adapter's product is formed apart and kept for its own rows only (so nothing of another
-// circuit's adapter, not even a NaN, reaches a row).
+// A row's arithmetic is the same in either kernel, whatever else its tile holds and however many rows a call covers: the
+// products of a row on the matrix cores do not see the other rows, T always comes from the same chain of 16x16 products, and
+// where rows of a tile differ in their adapter each adapter's product is formed apart and kept for its own rows only (so
+// nothing of another circuit's adapter, not even a NaN, reaches a row).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -20,16 +23,23 @@
 
 namespace {
 
+// Results leave past the caches, which are the weights' (2 % of the time)
+__device__ __forceinline__ void store_stream(void* p, const uint4& v)
+{
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), (u32x4*)p);
+}
+
 // Weights are the A operand of the 32x32 products and the rows the B operand, so that a lane's 16 accumulators belong to one
 // row; with column 16 hi + 4 a + b at operand row 8 a + 4 hi + b they are 16 neighbouring columns.
 __device__ __forceinline__ int column_of(int m) { return 16 * ((m >> 2) & 1) + 4 * (m >> 3) + (m & 3); }
 
-constexpr int GROUP = 3;                          // column tiles of 32 that a wave takes at a time
+// Calls of up to so many rows split the columns over workgroups
+constexpr int64_t SPREAD_ROWS = 4096;
 template <typename T> constexpr int PIECE = 16 / (int)sizeof(T);      // elements of 16 bytes
 inline int rank8(int rank) { return (rank + 7) / 8 * 8; }
 
-// W: unit ((group * KC + c) * GROUP + j) * 64 + lane holds rows k = (2c + lane/32) E .. + E-1 of column 32 (GROUP group + j) +
-// column_of(lane % 32). Down: per adapter, unit (k/E) * rank + n holds rows k .. k+E-1 of column n. Up: per adapter, unit
+// W: unit (tile * KC + c) * 64 + lane holds rows k = (2c + lane/32) E .. + E-1 of column 32 tile + column_of(lane % 32). Down: per adapter, unit (k/E) * rank + n holds rows k .. k+E-1 of column n. Up: per adapter, unit
 // (q/E) * 3D + column holds rows q .. q+E-1, zero from `rank` on (up to the next multiple of eight).
 template <typename T, int D>
 __global__ void lora_pack_kernel(dg4_lora_pack_args p)
@@ -42,9 +52,8 @@ __global__ void lora_pack_kernel(dg4_lora_pack_args p)
         T* dst;
         if (u < w_units) {
             const int lane = (int)(u & 63);
-            const int64_t t = u >> 6;
-            const int j = (int)(t % GROUP), c = (int)(t / GROUP % KC), group = (int)(t / GROUP / KC);
-            const int col = (group * GROUP + j) * 32 + column_of(lane & 31), k0 = (2 * c + (lane >> 5)) * E;
+            const int c = (int)((u >> 6) % KC), tile = (int)((u >> 6) / KC);
+            const int col = tile * 32 + column_of(lane & 31), k0 = (2 * c + (lane >> 5)) * E;
 #pragma unroll
             for (int i = 0; i < E; ++i) piece[i] = ((const T*)p.w)[(int64_t)(k0 + i) * (3 * D) + col];
             dst = (T*)p.w_packed + u * E;
@@ -70,242 +79,527 @@ __global__ void lora_pack_kernel(dg4_lora_pack_args p)
         for (int64_t a = threadIdx.x; a < p.n_adapters; a += blockDim.x) p.gain_packed[a] = p.gain ? p.gain[a] : 1.f;
 }
 
-// LDS of a workgroup, in bytes: the rows; T of every row; what is needed before T is finished (its two halves) and after it
-// (rows on their way out), one place.
-template <typename T, int D, int RT, int JT> struct Lds {
-    static constexpr int ROWS = RT * 32;
-    static constexpr int S_STRIDE = D + PIECE<T>;                                  // elements
-    static constexpr int O_STRIDE = JT * 32 + PIECE<T>;
-    static constexpr int S_BYTES = ROWS * S_STRIDE * (int)sizeof(T);
-    // T: bfloat16 keeps it as a sum of two (high and low part), so that the product with U_a loses nothing that the
-    // output's own rounding would not
-    __host__ __device__ static constexpr int t_stride(int r8) { return sizeof(T) == 2 ? 2 * r8 + 8 : r8 + 4; }
-    __host__ __device__ static constexpr int t_bytes(int r8) { return ROWS * t_stride(r8) * (int)sizeof(T); }
-    __host__ __device__ static constexpr int half_stride(int r8) { return (r8 + 31) / 32 * 32 + 4; }     // floats
-    static int bytes(int r8)
+constexpr int ROWS = 32;                          // rows of a product, and of a tile of the streaming kernel
+constexpr int RANKS = 8;                          // ranks per chunk of T U_a, either type
+
+// Rows of T in LDS, elements: bfloat16 keeps T as a sum of two (high parts, then low parts), so that the product with U_a
+// loses nothing that the output's own rounding would not
+template <typename T> __host__ __device__ constexpr int low_stride(int r8) { return sizeof(T) == 2 ? 2 * r8 + 8 : r8 + 4; }
+
+// One step of a 16x16 product: sixteen bytes of either operand, of row lane % 16 of each, part lane / 16 of the step's 4 E
+// elements; accumulator i of a lane is row 4 (lane / 16) + i of the first operand, row lane % 16 of the second.
+__device__ __forceinline__ void mma16(const uint4& a, const uint4& b, f32x4& c, bf16_t)
+{
+    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ void mma16(const uint4& a, const uint4& b, f32x4& c, float)
+{
+    c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.x), __uint_as_float(b.x), c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.y), __uint_as_float(b.y), c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.z), __uint_as_float(b.z), c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.w), __uint_as_float(b.w), c, 0, 0, 0);
+}
+
+// The sixteen columns of D_a from q0 on, as operand of all its steps
+template <typename T, int D> constexpr int DOWN_STEPS = D / (4 * PIECE<T>);
+template <typename T, int D>
+__device__ __forceinline__ void fetch_down(const dg4_lora_args& p, int a, int q0, int lane, uint4 (&d)[DOWN_STEPS<T, D>])
+{
+    // (columns behind the last rank are not used)
+    const uint4* src = (const uint4*)p.down_packed + ((int64_t)a * (D / PIECE<T>) + lane / 16) * p.rank + min(q0 + lane % 16, p.rank - 1);
+#pragma unroll
+    for (int k = 0; k < DOWN_STEPS<T, D>; ++k) d[k] = src[4 * k * p.rank];
+}
+// Sixteen rows of S (in LDS, `stride` elements apart) times sixteen columns of D_a: a lane has four columns of row lane % 16
+template <typename T, int D>
+__device__ __forceinline__ f32x4 down_product(const uint4 (&d)[DOWN_STEPS<T, D>], const T* rows, int stride, int lane)
+{
+    f32x4 sum = { 0.f, 0.f, 0.f, 0.f };
+    const T* row = rows + (lane % 16) * stride + lane / 16 * PIECE<T>;
+#pragma unroll
+    for (int k = 0; k < DOWN_STEPS<T, D>; ++k) mma16(d[k], *(const uint4*)(row + 4 * k * PIECE<T>), sum, T{});
+    return sum;
+}
+// A lane's four ranks q .. q + 3 of a row of T, into that row in LDS
+template <typename T> __device__ __forceinline__ void put_low(T* row, int q, int rank, int r8, const f32x4& sum, float gain)
+{
+    if (q >= r8) return;
+    float v[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = q + k < rank ? sum[k] * gain : 0.f;
+    if constexpr (sizeof(T) == 2) {
+        uint32_t h[4];
+        float rest[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            h[k] = f32_to_bf16_bits(v[k]);
+            const float back = __uint_as_float(h[k] << 16);
+            rest[k] = fabsf(back) < INFINITY ? v[k] - back : 0.f;                  // (an infinity has no low part)
+        }
+        *(uint2*)(row + q) = make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
+        *(uint2*)(row + r8 + q) = make_uint2(pack_bf16x2(rest[0], rest[1]), pack_bf16x2(rest[2], rest[3]));
+    } else {
+        *(float4*)(row + q) = make_float4(v[0], v[1], v[2], v[3]);
+    }
+}
+// T of sixteen rows whose adapters differ, ranks q0 .. q0 + 15: adapter after adapter, kept for its own rows
+template <typename T, int D>
+__device__ __forceinline__ f32x4 down_product_mixed(const dg4_lora_args& p, int mine, int q0, const T* rows, int stride, int lane)
+{
+    f32x4 kept = { 0.f, 0.f, 0.f, 0.f };
+    uint64_t todo = __ballot(mine >= 0);
+    while (todo) {
+        const int a = __builtin_amdgcn_readlane(mine, (int)__builtin_ctzll(todo));
+        todo &= ~__ballot(mine == a);
+        uint4 d[DOWN_STEPS<T, D>];
+        fetch_down<T, D>(p, a, q0, lane, d);
+        const f32x4 sum = down_product<T, D>(d, rows, stride, lane);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) kept[i] = mine == a ? sum[i] : kept[i];
+    }
+    return kept;
+}
+
+// The adapters of a wave's rows; a row has one or more lanes (-1: none).
+struct Adapters {
+    int mine, first;                              // this lane's row's; row 0's
+    bool any, one;                                // some row has one; all rows have the same
+    __device__ __forceinline__ void set(int id, int64_t n_adapters)
     {
-        return S_BYTES + t_bytes(r8) + std::max(2 * ROWS * half_stride(r8) * 4, 4 * 32 * O_STRIDE * (int)sizeof(T));
+        mine = id >= 0 && id < n_adapters ? id : -1;
+        first = __builtin_amdgcn_readfirstlane(mine);
+        any = __ballot(mine >= 0) != 0;
+        one = __ballot(mine != first) == 0;
     }
 };
 
-// A workgroup of four waves takes RT * 32 rows; a wave takes column tiles in passes of JT. SPREAD: one pass per wave, the
-// columns go to 3D/32/4 workgroups along y, and a tile holds p.tile_rows <= 32 rows (the rest of its operand repeats the
-// last): calls with few rows, where latency counts. Else the workgroup takes all columns.
-template <typename T, int D, int RT, int JT, bool SPREAD>
-__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void lora_proj_kernel(dg4_lora_args p)
+// T U_a for JT column tiles from `tile` on, into zeroed accumulators, two chunks of ranks at a time. A tile of rows with one
+// adapter has its first two chunks requested ahead, by first(). Otherwise adapter after adapter, a column tile at a time, the
+// next two chunks (of the same adapter or the next) requested before these are multiplied.
+template <typename T, int D, int JT> struct UpProduct {
+    uint4 up[2][JT];
+    template <int N>
+    __device__ __forceinline__ static void fetch(const dg4_lora_args& p, int a, int c0, int tile, int n, int hi, uint4 (&to)[2][N])
+    {
+        constexpr int E = PIECE<T>;
+        const int chunks = p.rank8 / RANKS;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const int at = min(c0 + c, chunks - 1), unit = sizeof(T) == 2 ? at : 2 * at + hi;
+            const uint4* src = (const uint4*)p.up_packed + ((int64_t)a * (p.rank8 / E) + unit) * (3 * D) + tile * 32 + column_of(n);
+#pragma unroll
+            for (int j = 0; j < N; ++j) to[c][j] = src[j * 32];
+        }
+    }
+    __device__ __forceinline__ void first(const dg4_lora_args& p, const Adapters& ad, int tile, int n, int hi)
+    {
+        if (ad.any && ad.one) fetch(p, ad.first, 0, tile, n, hi, up);
+    }
+    // chunk c of T as operand: bfloat16 has the high parts of eight ranks in one half of the wave and their low parts in the
+    // other, against the same eight rows of U_a
+    __device__ __forceinline__ static uint4 low_operand(const dg4_lora_args& p, const T* low, int c, int n, int hi)
+    {
+        const T* row = low + n * low_stride<T>(p.rank8);
+        return *(const uint4*)(sizeof(T) == 2 ? row + hi * p.rank8 + c * 8 : row + (2 * c + hi) * 4);
+    }
+    __device__ __forceinline__ void run_one(const dg4_lora_args& p, const Adapters& ad, const T* low, int tile, int n, int hi, f32x16 (&acc)[JT])
+    {
+        const int chunks = p.rank8 / RANKS;
+        for (int c0 = 0; c0 < chunks; c0 += 2) {
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                if (c0 + c < chunks) {
+                    const uint4 b = low_operand(p, low, c0 + c, n, hi);
+#pragma unroll
+                    for (int j = 0; j < JT; ++j) Mma<T>::run(up[c][j], b, acc[j]);
+                }
+            }
+            if (c0 + 2 < chunks) fetch(p, ad.first, c0 + 2, tile, n, hi, up);
+        }
+    }
+    __device__ __forceinline__ static void run_mixed(const dg4_lora_args& p, const Adapters& ad, const T* low, int tile, int n, int hi, f32x16 (&acc)[JT])
+    {
+        const int chunks = p.rank8 / RANKS;
+#pragma unroll
+        for (int j = 0; j < JT; ++j) {
+            uint64_t todo = __ballot(ad.mine >= 0);
+            int a = __builtin_amdgcn_readlane(ad.mine, (int)__builtin_ctzll(todo));
+            todo &= ~__ballot(ad.mine == a);
+            uint4 now[2][1], next[2][1];
+            fetch(p, a, 0, tile + j, n, hi, now);
+            f32x16 part;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) part[i] = 0.f;
+            for (int c0 = 0;;) {
+                const bool ends = c0 + 2 >= chunks, more = !ends || todo != 0;
+                const int a_next = ends && todo ? __builtin_amdgcn_readlane(ad.mine, (int)__builtin_ctzll(todo)) : a;
+                if (more) fetch(p, a_next, ends ? 0 : c0 + 2, tile + j, n, hi, next);
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+                    if (c0 + c < chunks) Mma<T>::run(now[c][0], low_operand(p, low, c0 + c, n, hi), part);
+                if (ends) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) { acc[j][i] = ad.mine == a ? part[i] : acc[j][i]; part[i] = 0.f; }
+                }
+                if (!more) break;
+                now[0][0] = next[0][0]; now[1][0] = next[1][0];
+                c0 = ends ? 0 : c0 + 2;
+                todo &= ~__ballot(ad.mine == a_next);
+                a = a_next;
+            }
+        }
+    }
+};
+
+// Where Q, K and V go: K's distance from Q and V's from K, to be added by mask. (Chosen with ?: per lane, the address is loaded
+// from the kernel's arguments, or from the stack, for every store, and every store waits for those before it.)
+struct Outputs {
+    uint64_t q, k_q, v_k;
+    __device__ __forceinline__ explicit Outputs(const dg4_lora_args& p)
+        : q((uint64_t)p.out[0]), k_q((uint64_t)p.out[1] - (uint64_t)p.out[0]), v_k((uint64_t)p.out[2] - (uint64_t)p.out[1]) {}
+    template <typename T, int D> __device__ __forceinline__ T* at(int64_t row, int col) const
+    {
+        const uint64_t base = q + (k_q & (uint64_t)((int64_t)(D - 1 - col) >> 63)) + (v_k & (uint64_t)((int64_t)(2 * D - 1 - col) >> 63));
+        return (T*)base + row * D + col % D;
+    }
+};
+
+// JT finished column tiles of the wave's rows, through its own corner of LDS (a wave's LDS operations complete in order), as
+// 16-byte pieces of rows to Q, K or V
+template <typename T, int D, int JT, int STRIDE>
+__device__ __forceinline__ void put_tiles(const Outputs& to, const f32x16* acc, T* out_rows, int64_t r0, int64_t r_end, int tile, int lane)
 {
-    using L = Lds<T, D, RT, JT>;
-    constexpr int E = PIECE<T>, KC = D / (2 * E), TILES = 3 * D / 32;
-    constexpr int PASSES = SPREAD ? 1 : TILES / 4 / JT;
-    static_assert(SPREAD ? JT == 1 && RT == 1 : JT == GROUP && TILES % (4 * JT) == 0, "column tiles");
-    constexpr int RING = 4;                       // chunks of weights requested ahead
+    constexpr int E = PIECE<T>, PPR = JT * 32 / E;             // pieces per row
+    const int n = lane & 31, hi = lane >> 5;
+#pragma unroll
+    for (int j = 0; j < JT; ++j) {
+        uint4* dst = (uint4*)(out_rows + n * STRIDE + j * 32 + 16 * hi);
+        const f32x16& x = acc[j];
+        if constexpr (sizeof(T) == 2) {
+            dst[0] = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+            dst[1] = make_uint4(pack_bf16x2(x[8], x[9]), pack_bf16x2(x[10], x[11]), pack_bf16x2(x[12], x[13]), pack_bf16x2(x[14], x[15]));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                dst[i] = make_uint4(__float_as_uint(x[4 * i]), __float_as_uint(x[4 * i + 1]), __float_as_uint(x[4 * i + 2]), __float_as_uint(x[4 * i + 3]));
+        }
+    }
+    constexpr int PIECES = ROWS * PPR / 64;
+    uint4 v[PIECES];
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) v[i] = *((const uint4*)(out_rows + (lane + 64 * i) / PPR * STRIDE) + (lane + 64 * i) % PPR);
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        const int piece = lane + 64 * i, row = piece / PPR, cc = piece % PPR;
+        if (r0 + row < r_end) store_stream(to.at<T, D>(r0 + row, tile * 32 + cc * E), v[i]);
+    }
+}
+
+// LDS of the streaming kernel, in bytes: the rows, T, rows on their way out
+template <typename T, int D, int TILES_OUT> struct StreamLds {
+    static constexpr int S_STRIDE = D + PIECE<T>;                                  // elements
+    static constexpr int S_BYTES = ROWS * S_STRIDE * (int)sizeof(T);
+    static constexpr int O_STRIDE = TILES_OUT * 32 + PIECE<T>;
+    __host__ __device__ static constexpr int out_at(int r8) { return S_BYTES + ROWS * low_stride<T>(r8) * (int)sizeof(T); }
+    __host__ __device__ static constexpr int bytes(int r8) { return out_at(r8) + 4 * ROWS * O_STRIDE * (int)sizeof(T); }
+};
+
+// A workgroup of four waves takes a tile of rows, a wave JT column tiles at a time. SPREAD, for calls with few rows, where latency
+// counts: a wave takes one column tile, the others go to 3D/32/4 workgroups along y, and a tile holds p.tile_rows <= 32
+// rows (the rest of its operand repeats the last).
+template <typename T, int D, int JT, bool SPREAD>
+__global__ __launch_bounds__(256, 2) void lora_stream_kernel(dg4_lora_args p)
+{
+    constexpr int E = PIECE<T>, KC = D / (2 * E), TILES = 3 * D / 32, PASSES = SPREAD ? 1 : TILES / 4 / JT;
+    static_assert(SPREAD ? JT == 1 : TILES % (4 * JT) == 0, "column tiles");
+    constexpr int TILES_OUT = sizeof(T) == 2 ? JT : 1;         // column tiles that leave together (128 bytes of a row)
+    using L = StreamLds<T, D, TILES_OUT>;
+    constexpr int RING = sizeof(T) == 2 ? 8 : 4;  // chunks of weights requested ahead
+    static_assert(KC % RING == 0, "the ring's place of a chunk is the same in every pass");
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 31, hi = lane >> 5;
-    const int tile_rows = SPREAD ? p.tile_rows : L::ROWS;
+    const int tile_rows = SPREAD ? p.tile_rows : ROWS;
     const int64_t r0 = p.row_begin + (int64_t)blockIdx.x * tile_rows;
     const int64_t r_end = min(p.row_end, r0 + tile_rows);
     auto row_at = [&](int i) { const int64_t r = r0 + i; return r < r_end ? r : r_end - 1; };
 
     T* const rows = (T*)smem;
     T* const low = (T*)(smem + L::S_BYTES);
-    float* const half_sum = (float*)(smem + L::S_BYTES + L::t_bytes(p.rank8));
-    T* const out_rows = (T*)half_sum + wave * 32 * L::O_STRIDE;
+    T* const out_rows = (T*)(smem + L::out_at(p.rank8)) + wave * ROWS * L::O_STRIDE;
 
-    // this wave's weights: a linear stream over its passes
+    // Requests, in the order in which they are waited for: the rows' adapters, the rows, the first chunks of weights
+    const int id = p.adapter ? p.adapter[row_at(n)] : -1;
+    constexpr int CPR = D / E, PIECES = ROWS * CPR / 256;
+    uint4 row_piece[PIECES];
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        const int piece = (int)threadIdx.x + 256 * i;
+        row_piece[i] = *((const uint4*)((const T*)p.s + row_at(piece / CPR) * D) + piece % CPR);
+    }
     const int tile0 = SPREAD ? (int)blockIdx.y * 4 + wave : wave * PASSES * JT;
-    const uint4* wp = (const uint4*)p.w_packed + ((int64_t)(tile0 / GROUP) * KC * GROUP + tile0 % GROUP) * 64 + lane;
-    auto weight = [&](int f) { return wp[(int64_t)(SPREAD ? f * GROUP : f) * 64]; };      // f = chunk * JT + j, on through the passes
-    {
-        constexpr int CPR = D / E;
-        uint4 v[L::ROWS * CPR / 256];
-#pragma unroll
-        for (int i = 0; i < L::ROWS * CPR / 256; ++i) {
-            const int piece = (int)threadIdx.x + 256 * i;
-            v[i] = *((const uint4*)((const T*)p.s + row_at(piece / CPR) * D) + piece % CPR);
-        }
-#pragma unroll
-        for (int i = 0; i < L::ROWS * CPR / 256; ++i) {
-            const int piece = (int)threadIdx.x + 256 * i;
-            *((uint4*)(rows + (piece / CPR) * L::S_STRIDE) + piece % CPR) = v[i];
-        }
-    }
-    // adapter of this lane's row of each row tile (-1: none)
-    int ad[RT];
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-        ad[t] = p.adapter ? p.adapter[row_at(t * 32 + n)] : -1;
-        if (ad[t] < 0 || ad[t] >= p.n_adapters) ad[t] = -1;
-    }
-    uint64_t any = 0;
-    bool one = true;                              // one adapter for the whole tile
-    const int first_ad = __builtin_amdgcn_readfirstlane(ad[0]);
-#pragma unroll
-    for (int t = 0; t < RT; ++t) { any |= __ballot(ad[t] >= 0); one = one && __ballot(ad[t] != first_ad) == 0; }
-    __syncthreads();
-
-    if (any) {
-        // T, by (row tile, half of the features): waves 0 .. 2 RT - 1
-        if (wave < 2 * RT) {
-            const int t = wave >> 1, half = wave & 1;
-            int mine = ad[0];
-#pragma unroll
-            for (int q = 1; q < RT; ++q) mine = t == q ? ad[q] : mine;
-            uint64_t todo = __ballot(mine >= 0);
-            while (todo) {
-                const int a = __builtin_amdgcn_readlane(mine, (int)__builtin_ctzll(todo));
-                todo &= ~__ballot(mine == a);
-                const uint4* dp = (const uint4*)p.down_packed + (int64_t)a * (D / E) * p.rank;
-                for (int nt = 0; nt * 32 < p.rank; ++nt) {
-                    const int col = nt * 32 + column_of(n);
-                    uint4 d[KC / 2];
-#pragma unroll
-                    for (int c = 0; c < KC / 2; ++c)
-                        d[c] = col < p.rank ? dp[(int64_t)(2 * (half * (KC / 2) + c) + hi) * p.rank + col] : make_uint4(0, 0, 0, 0);
-                    f32x16 acc;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) acc[i] = 0.f;
-#pragma unroll
-                    for (int c = 0; c < KC / 2; ++c)
-                        Mma<T>::run(d[c], *(const uint4*)(rows + (t * 32 + n) * L::S_STRIDE + (2 * (half * (KC / 2) + c) + hi) * E), acc);
-                    if (mine == a) {
-                        float4* dst = (float4*)(half_sum + (half * L::ROWS + t * 32 + n) * L::half_stride(p.rank8) + nt * 32 + 16 * hi);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) dst[i] = make_float4(acc[4 * i], acc[4 * i + 1], acc[4 * i + 2], acc[4 * i + 3]);
-                    }
-                }
-            }
-        }
-        __syncthreads();
-        for (int i = threadIdx.x; i < L::ROWS * (p.rank8 / 4); i += 256) {
-            const int row = i % L::ROWS, q0 = i / L::ROWS * 4;
-            const float* h0 = half_sum + row * L::half_stride(p.rank8) + q0;
-            const float* h1 = h0 + L::ROWS * L::half_stride(p.rank8);
-            const int a = p.adapter[row_at(row)];
-            const bool has = a >= 0 && a < p.n_adapters;
-            const float gain = has ? p.gain_packed[a] : 0.f;
-            float v[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] = has && q0 + k < p.rank ? (h0[k] + h1[k]) * gain : 0.f;
-            T* dst = low + row * L::t_stride(p.rank8) + q0;
-            if constexpr (sizeof(T) == 2) {
-                uint32_t h[4];
-                float rest[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    h[k] = f32_to_bf16_bits(v[k]);
-                    const float back = __uint_as_float(h[k] << 16);
-                    rest[k] = fabsf(back) < INFINITY ? v[k] - back : 0.f;
-                }
-                *(uint2*)dst = make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
-                *(uint2*)(dst + p.rank8) = make_uint2(pack_bf16x2(rest[0], rest[1]), pack_bf16x2(rest[2], rest[3]));
-            } else {
-                *(float4*)dst = make_float4(v[0], v[1], v[2], v[3]);
-            }
-        }
-        __syncthreads();
-    }
-    // chunk c of T as operand: bfloat16 has the high parts of eight ranks in one half of the wave and their low parts in
-    // the other, against the same eight rows of U_a
-    constexpr int RANKS = 8;                      // ranks per chunk, either type
-    const int chunks = p.rank8 / RANKS;
-    auto low_at = [&](int t, int c) {
-        const T* row = low + (t * 32 + n) * L::t_stride(p.rank8);
-        return *(const uint4*)(sizeof(T) == 2 ? row + hi * p.rank8 + c * 8 : row + (2 * c + hi) * 4);
-    };
-    auto up_at = [&](int a, int c, int tile) {
-        const int64_t unit = sizeof(T) == 2 ? c : 2 * c + hi;
-        return ((const uint4*)p.up_packed)[((int64_t)a * (p.rank8 / E) + unit) * (3 * D) + tile * 32 + column_of(n)];
-    };
-
+    const uint4* wp = (const uint4*)p.w_packed + (int64_t)tile0 * KC * 64 + lane;
     uint4 ring[RING][JT];
 #pragma unroll
     for (int c = 0; c < RING; ++c)
 #pragma unroll
-        for (int j = 0; j < JT; ++j) ring[c][j] = weight(c * JT + j);
-#pragma unroll 1
-    for (int pass = 0; pass < PASSES; ++pass) {
-        f32x16 acc[RT][JT];
+        for (int j = 0; j < JT; ++j) ring[c][j] = wp[(j * KC + c) * 64];
+
+    Adapters ad;
+    ad.set(id, p.n_adapters);
+    // T: waves 0 and 2 take rows 0 .. 15, waves 1 and 3 rows 16 .. 31, each every second sixteen ranks
+    const int half = wave & 1;
+    Adapters ad16;
+    ad16.set(__shfl(ad.mine, half * 16 + lane % 16), p.n_adapters);
+    const bool down_ahead = ad16.any && ad16.one && wave / 2 * 16 < p.rank;
+    uint4 d[DOWN_STEPS<T, D>];
+    if (down_ahead) fetch_down<T, D>(p, ad16.first, wave / 2 * 16, lane, d);
+    UpProduct<T, D, JT> up;
+    up.first(p, ad, tile0, n, hi);
+    const float gain = ad16.mine >= 0 ? p.gain_packed[ad16.mine] : 0.f;
 #pragma unroll
-        for (int t = 0; t < RT; ++t)
-#pragma unroll
-            for (int j = 0; j < JT; ++j)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) acc[t][j][i] = 0.f;
-        const int tile = tile0 + pass * JT;
-        if (any && one) {
-            for (int c = 0; c < chunks; ++c) {
-                uint4 u[JT];
-#pragma unroll
-                for (int j = 0; j < JT; ++j) u[j] = up_at(first_ad, c, tile + j);
-#pragma unroll
-                for (int t = 0; t < RT; ++t) {
-                    const uint4 b = low_at(t, c);
-#pragma unroll
-                    for (int j = 0; j < JT; ++j) Mma<T>::run(u[j], b, acc[t][j]);
-                }
+    for (int i = 0; i < PIECES; ++i) {
+        const int piece = (int)threadIdx.x + 256 * i;
+        *((uint4*)(rows + (piece / CPR) * L::S_STRIDE) + piece % CPR) = row_piece[i];
+    }
+    __syncthreads();
+    if (ad.any) {
+        for (int q0 = wave / 2 * 16; ad16.any && q0 < p.rank; q0 += 32) {
+            const T* mine = rows + half * 16 * L::S_STRIDE;
+            f32x4 sum;
+            if (ad16.one) {
+                if (q0 >= 32) fetch_down<T, D>(p, ad16.first, q0, lane, d);
+                sum = down_product<T, D>(d, mine, L::S_STRIDE, lane);
+            } else {
+                sum = down_product_mixed<T, D>(p, ad16.mine, q0, mine, L::S_STRIDE, lane);
             }
-        } else if (any) {
-#pragma unroll
-            for (int t = 0; t < RT; ++t) {
-                uint64_t todo = __ballot(ad[t] >= 0);
-                while (todo) {
-                    const int a = __builtin_amdgcn_readlane(ad[t], (int)__builtin_ctzll(todo));
-                    todo &= ~__ballot(ad[t] == a);
-#pragma unroll
-                    for (int j = 0; j < JT; ++j) {
-                        f32x16 part;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) part[i] = 0.f;
-                        for (int c = 0; c < chunks; ++c) Mma<T>::run(up_at(a, c, tile + j), low_at(t, c), part);
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) acc[t][j][i] = ad[t] == a ? part[i] : acc[t][j][i];
-                    }
-                }
-            }
+            // (rows without an adapter get, or have, what is kept for no row)
+            put_low<T>(low + (half * 16 + lane % 16) * low_stride<T>(p.rank8), q0 + lane / 16 * 4, p.rank, p.rank8, sum, gain);
         }
+        __syncthreads();
+    }
+    const Outputs outputs(p);
+    auto row_operand = [&](int c) __attribute__((always_inline)) { return *(const uint4*)(rows + n * L::S_STRIDE + (2 * c + hi) * E); };
+    // (unrolled, so that the weights on their way are waited for one by one and not behind the stores of a pass)
+#pragma unroll
+    for (int pass = 0; pass < PASSES; ++pass) {
+        f32x16 acc[JT];
+#pragma unroll
+        for (int j = 0; j < JT; ++j)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[j][i] = 0.f;
+        const int tile = tile0 + pass * JT;
+        if (ad.any) {
+            if (ad.one) up.run_one(p, ad, low, tile, n, hi, acc);
+            else up.run_mixed(p, ad, low, tile, n, hi, acc);
+        }
+        if (pass + 1 < PASSES) up.first(p, ad, tile + JT, n, hi);
+        uint4 b[2];                               // rows as operand: this chunk's and the next's
+        b[0] = row_operand(0);
 #pragma unroll
         for (int c = 0; c < KC; ++c) {
-            uint4 b[RT];
+            if (c + 1 < KC) b[(c + 1) & 1] = row_operand(c + 1);
 #pragma unroll
-            for (int t = 0; t < RT; ++t) b[t] = *(const uint4*)(rows + (t * 32 + n) * L::S_STRIDE + (2 * c + hi) * E);
+            for (int j = 0; j < JT; ++j) Mma<T>::run(ring[c % RING][j], b[c & 1], acc[j]);
+            const int ahead = pass * KC + c + RING;            // chunk, on through the passes
+            if (ahead < PASSES * KC) {
+#pragma unroll
+                for (int j = 0; j < JT; ++j) ring[c % RING][j] = wp[((ahead / KC * JT + j) * KC + ahead % KC) * 64];
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int j = 0; j < JT; j += TILES_OUT) put_tiles<T, D, TILES_OUT, L::O_STRIDE>(outputs, acc + j, out_rows, r0, r_end, tile + j, lane);
+    }
+}
+
+// LDS of the resident kernel, in bytes: two buffers each of the rows of a tile, of their T and of their adapters; U_a of
+// this workgroup's columns; rows on their way out
+template <int D, int JT> struct WalkLds {
+    static constexpr int TILE = 64;
+    static constexpr int S_STRIDE = D + 8;                                         // elements
+    static constexpr int S_BYTES = TILE * S_STRIDE * 2;
+    static constexpr int O_STRIDE = JT * 32 + 8;
+    __host__ __device__ static constexpr int low_bytes(int r8) { return TILE * low_stride<bf16_t>(r8) * 2; }
+    __host__ __device__ static constexpr int ids_at(int r8) { return 2 * (S_BYTES + low_bytes(r8)); }
+    __host__ __device__ static constexpr int up_at(int r8) { return ids_at(r8) + 2 * TILE * 4; }
+    // (operand units of 16 bytes: [wave][chunk][column tile][32])
+    __host__ __device__ static constexpr int out_at(int r8) { return up_at(r8) + 4 * (r8 / RANKS) * JT * 32 * 16; }
+    __host__ __device__ static constexpr int bytes(int r8) { return out_at(r8) + 4 * ROWS * O_STRIDE * 2; }
+};
+
+// bfloat16, many rows. A workgroup of eight waves per compute unit keeps its share of W in the registers of four of them, JT
+// column tiles each: all columns at hidden 128 (96 registers), one of Q, K and V at 256 (128 registers; PARTS = 3; the
+// workgroups of one walk sit on one XCD, so that the rows come from memory once). These four multiply and store and wait for
+// no load; U_a sits in LDS until the adapter changes. The other four, sixteen rows each, request the rows two tiles ahead,
+// put the next tile's into LDS and form their T, with D_a in registers until the adapter changes. One barrier per tile.
+template <int D, int PARTS>
+__global__ __launch_bounds__(512, 2) void lora_resident_kernel(dg4_lora_args p)
+{
+    typedef bf16_t T;
+    constexpr int E = PIECE<T>, KC = D / (2 * E), JT = 3 * D / 32 / PARTS / 4;
+    using L = WalkLds<D, JT>;
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = lane & 31, hi = lane >> 5;
+    // workgroups go to the eight XCDs in turn
+    const int xcd = (int)blockIdx.x & 7, slot = (int)blockIdx.x >> 3, walks = (int)(gridDim.x / (8 * PARTS)) * 8;
+    const int share = slot % PARTS, walk = slot / PARTS * 8 + xcd;
+    const int64_t tiles = (p.row_end - p.row_begin + L::TILE - 1) / L::TILE;
+    const int64_t steps = walk < tiles ? (tiles - walk + walks - 1) / walks : 0;   // tiles walk, walk + walks, ...
+    if (steps == 0) return;
+    auto rows_of = [&](int64_t step) { return (T*)(smem + (step & 1) * L::S_BYTES); };
+    auto low_of = [&](int64_t step) { return (T*)(smem + 2 * L::S_BYTES + (step & 1) * L::low_bytes(p.rank8)); };
+    auto ids_of = [&](int64_t step) { return (int*)(smem + L::ids_at(p.rank8)) + (step & 1) * L::TILE; };
+
+    if (wave >= 4) {
+        // rows 16 h .. 16 h + 15 of every tile
+        const int h = wave - 4;
+        constexpr int CPR = D / E, RPL = 64 / CPR, LOADS = 16 / RPL;               // rows per load instruction; a wave's loads of a tile
+        typedef uint32_t Pieces __attribute__((ext_vector_type(4 * LOADS)));       // (an array was kept in scratch memory)
+        struct Ahead { Pieces piece; int id; };
+        auto request = [&](int64_t step, Ahead& to) __attribute__((always_inline)) {
+            const int64_t r0 = p.row_begin + (walk + step * walks) * L::TILE + 16 * h;
+            auto row_at = [&](int i) { return min(r0 + i, p.row_end - 1); };
+            to.id = p.adapter ? p.adapter[row_at(lane % 16)] : -1;
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                const uint4 v = *((const uint4*)((const T*)p.s + row_at(i * RPL + lane / CPR) * D) + lane % CPR);
+                to.piece[4 * i] = v.x; to.piece[4 * i + 1] = v.y; to.piece[4 * i + 2] = v.z; to.piece[4 * i + 3] = v.w;
+            }
+        };
+        uint4 d[DOWN_STEPS<T, D>];
+        int held = -1;                            // the adapter whose first sixteen ranks d holds
+        auto put = [&](int64_t step, const Ahead& from) __attribute__((always_inline)) {
+            Adapters ad;
+            ad.set(from.id, p.n_adapters);
+            const float gain = ad.mine >= 0 ? p.gain_packed[ad.mine] : 0.f;
+            if (ad.any && ad.one && ad.first != held) { fetch_down<T, D>(p, ad.first, 0, lane, d); held = ad.first; }
+            T* const rows = rows_of(step) + 16 * h * L::S_STRIDE;
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i)
+                *((uint4*)(rows + (i * RPL + lane / CPR) * L::S_STRIDE) + lane % CPR) =
+                    make_uint4(from.piece[4 * i], from.piece[4 * i + 1], from.piece[4 * i + 2], from.piece[4 * i + 3]);
+            if (lane < 16) ids_of(step)[16 * h + lane] = ad.mine;
+            if (!ad.any) return;
+            // (the rows are this wave's own: its LDS operations complete in order)
+            T* const low = low_of(step) + (16 * h + lane % 16) * low_stride<T>(p.rank8);
+            for (int q0 = 0; q0 < p.rank; q0 += 16) {
+                f32x4 sum;
+                if (!ad.one) {
+                    sum = down_product_mixed<T, D>(p, ad.mine, q0, rows, L::S_STRIDE, lane);
+                } else if (q0 == 0) {
+                    sum = down_product<T, D>(d, rows, L::S_STRIDE, lane);
+                } else {
+                    uint4 more[DOWN_STEPS<T, D>];
+                    fetch_down<T, D>(p, ad.first, q0, lane, more);
+                    sum = down_product<T, D>(more, rows, L::S_STRIDE, lane);
+                }
+                put_low<T>(low, q0 + lane / 16 * 4, p.rank, p.rank8, sum, gain);
+            }
+        };
+        Ahead even, odd;
+        request(0, even);
+        if (steps > 1) request(1, odd);
+        put(0, even);
+        if (steps > 2) request(2, even);
+        __syncthreads();
+        for (int64_t step = 0; step < steps; step += 2) {
+            // while tile `step` is multiplied
+            if (step + 1 < steps) put(step + 1, odd);
+            if (step + 3 < steps) request(step + 3, odd);
+            __syncthreads();
+            if (step + 1 >= steps) return;
+            if (step + 2 < steps) put(step + 2, even);
+            if (step + 4 < steps) request(step + 4, even);
+            __syncthreads();
+        }
+        return;
+    }
+
+    const Outputs outputs(p);
+    const int tile0 = (share * 4 + wave) * JT;
+    uint4 w[JT][KC];
+    {
+        const uint4* wp = (const uint4*)p.w_packed + (int64_t)tile0 * KC * 64 + lane;
+#pragma unroll
+        for (int j = 0; j < JT; ++j)
+#pragma unroll
+            for (int c = 0; c < KC; ++c) w[j][c] = wp[(j * KC + c) * 64];
+        // (used here, so that they are waited for here and not, behind the stores of the step before, in every step)
+        typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+        for (int j = 0; j < JT; ++j)
+#pragma unroll
+            for (int c = 0; c < KC; ++c) {
+                u32x4 pin = __builtin_bit_cast(u32x4, w[j][c]);
+                __asm__ volatile("" : "+v"(pin));
+                w[j][c] = __builtin_bit_cast(uint4, pin);
+            }
+    }
+    const int chunks = p.rank8 / RANKS;
+    uint4* const up_held = (uint4*)(smem + L::up_at(p.rank8)) + wave * chunks * JT * 32;     // this wave's columns
+    int held = -1;                                // the adapter it holds
+    T* const out_rows = (T*)(smem + L::out_at(p.rank8)) + wave * ROWS * L::O_STRIDE;
+    __syncthreads();
+    for (int64_t step = 0; step < steps; ++step) {
+        const int64_t tile_r0 = p.row_begin + (walk + step * walks) * L::TILE;
+#pragma unroll 1
+        for (int t = 0; t < L::TILE / ROWS; ++t) {
+            const int64_t r0 = tile_r0 + t * ROWS, r_end = min(p.row_end, r0 + ROWS);
+            if (r0 >= r_end) break;
+            const T* rows = rows_of(step) + t * ROWS * L::S_STRIDE;
+            const T* low = low_of(step) + t * ROWS * low_stride<T>(p.rank8);
+            Adapters ad;
+            ad.set(ids_of(step)[t * ROWS + n], p.n_adapters);
+            f32x16 acc[JT];
 #pragma unroll
             for (int j = 0; j < JT; ++j)
 #pragma unroll
-                for (int t = 0; t < RT; ++t) Mma<T>::run(ring[c % RING][j], b[t], acc[t][j]);
-            if (c + RING < KC || pass + 1 < PASSES) {
+                for (int i = 0; i < 16; ++i) acc[j][i] = 0.f;
+            if (ad.any && !ad.one) {
+                UpProduct<T, D, JT>::run_mixed(p, ad, low, tile0, n, hi, acc);
+            } else if (ad.any) {
+                if (ad.first != held) {           // (32 lanes a column tile: either half of the wave multiplies the same rows of U_a)
+                    held = ad.first;
+                    for (int c = hi; c < chunks; c += 2)
 #pragma unroll
-                for (int j = 0; j < JT; ++j) ring[c % RING][j] = weight((pass * KC + c + RING) * JT + j);
-            }
-        }
-        // out through this wave's own corner of LDS (its operations complete in order), as 16-byte pieces of rows
-        constexpr int PPR = JT * 32 / E;          // pieces per row
+                        for (int j = 0; j < JT; ++j)
+                            up_held[(c * JT + j) * 32 + n] = ((const uint4*)p.up_packed)[((int64_t)held * chunks + c) * (3 * D) + (tile0 + j) * 32 + column_of(n)];
+                }
+                for (int c0 = 0; c0 < chunks; c0 += 2) {
+                    uint4 low_piece[2], up_piece[2][JT];
 #pragma unroll
-        for (int t = 0; t < RT; ++t) {
+                    for (int c = 0; c < 2; ++c) {
+                        const int at = min(c0 + c, chunks - 1);
+                        low_piece[c] = UpProduct<T, D, JT>::low_operand(p, low, at, n, hi);
 #pragma unroll
-            for (int j = 0; j < JT; ++j) {
-                uint4* dst = (uint4*)(out_rows + n * L::O_STRIDE + j * 32 + 16 * hi);
-                const f32x16& x = acc[t][j];
-                if constexpr (sizeof(T) == 2) {
-                    dst[0] = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
-                    dst[1] = make_uint4(pack_bf16x2(x[8], x[9]), pack_bf16x2(x[10], x[11]), pack_bf16x2(x[12], x[13]), pack_bf16x2(x[14], x[15]));
-                } else {
+                        for (int j = 0; j < JT; ++j) up_piece[c][j] = up_held[(at * JT + j) * 32 + n];
+                    }
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        dst[i] = make_uint4(__float_as_uint(x[4 * i]), __float_as_uint(x[4 * i + 1]), __float_as_uint(x[4 * i + 2]), __float_as_uint(x[4 * i + 3]));
+                    for (int c = 0; c < 2; ++c)
+                        if (c0 + c < chunks) {
+#pragma unroll
+                            for (int j = 0; j < JT; ++j) Mma<T>::run(up_piece[c][j], low_piece[c], acc[j]);
+                        }
                 }
             }
+            constexpr int WINDOW = 4;             // rows as operand: this chunk's and the next three's
+            uint4 b[WINDOW];
 #pragma unroll
-            for (int i = 0; i < 32 * PPR / 64; ++i) {
-                const int piece = lane + 64 * i, row = piece / PPR, cc = piece % PPR;
-                const uint4 v = *((const uint4*)(out_rows + row * L::O_STRIDE) + cc);
-                const int col = tile * 32 + cc * E;
-                const int64_t r = r0 + t * 32 + row;
-                T* dst = (T*)(col < D ? p.out[0] : col < 2 * D ? p.out[1] : p.out[2]);
-                if (r < r_end) *(uint4*)(dst + r * D + col % D) = v;
+            for (int c = 0; c < WINDOW - 1; ++c) b[c] = *(const uint4*)(rows + n * L::S_STRIDE + (2 * c + hi) * E);
+#pragma unroll
+            for (int c = 0; c < KC; ++c) {
+                if (c + WINDOW - 1 < KC) b[(c + WINDOW - 1) % WINDOW] = *(const uint4*)(rows + n * L::S_STRIDE + (2 * (c + WINDOW - 1) + hi) * E);
+#pragma unroll
+                for (int j = 0; j < JT; ++j) Mma<T>::run(w[j][c], b[c % WINDOW], acc[j]);
+                __builtin_amdgcn_sched_barrier(0);
             }
+            put_tiles<T, D, JT, L::O_STRIDE>(outputs, acc, out_rows, r0, r_end, tile0, lane);
         }
+        __syncthreads();
     }
 }
 
@@ -329,21 +623,31 @@ template <typename T, int D>
 int launch_proj(dg4_lora_args a, hipStream_t s)
 {
     const int64_t rows = a.row_end - a.row_begin;
-    if (rows <= 4096) {
-        using L = Lds<T, D, 1, 1>;
-        const auto kernel = lora_proj_kernel<T, D, 1, 1, true>;
+    if (rows <= SPREAD_ROWS) {
+        const auto kernel = lora_stream_kernel<T, D, 1, true>;
         // rows per tile: few enough for two workgroups per compute unit
         a.tile_rows = 1;
-        while (a.tile_rows < 32 && rows * (3 * D / 128) > (int64_t)512 * a.tile_rows) a.tile_rows *= 2;
-        const int smem = L::bytes(a.rank8);
+        while (a.tile_rows < ROWS && rows * (3 * D / 128) > (int64_t)512 * a.tile_rows) a.tile_rows *= 2;
+        const int smem = StreamLds<T, D, 1>::bytes(a.rank8);
         if (const int e = allow_lds(kernel, smem); e != hipSuccess) return e;
         hipLaunchKernelGGL(kernel, dim3((unsigned)((rows + a.tile_rows - 1) / a.tile_rows), 3 * D / 128), dim3(256), smem, s, a);
-    } else {
-        using L = Lds<T, D, 2, GROUP>;
-        const auto kernel = lora_proj_kernel<T, D, 2, GROUP, false>;
+    } else if constexpr (sizeof(T) == 2) {
+        constexpr int PARTS = D == 256 ? 3 : 1;
+        using L = WalkLds<D, 3 * D / 128 / PARTS>;
+        const auto kernel = lora_resident_kernel<D, PARTS>;
         const int smem = L::bytes(a.rank8);
         if (const int e = allow_lds(kernel, smem); e != hipSuccess) return e;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)((rows + L::ROWS - 1) / L::ROWS)), dim3(256), smem, s, a);
+        int dev = 0, cus = 0;
+        if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess) return hipErrorInvalidDevice;
+        // one workgroup per compute unit, as whole walks on every XCD
+        const int64_t walks = std::max<int64_t>(1, std::min<int64_t>(cus / (8 * PARTS), ((rows + L::TILE - 1) / L::TILE + 7) / 8));
+        hipLaunchKernelGGL(kernel, dim3((unsigned)(8 * PARTS * walks)), dim3(512), smem, s, a);
+    } else {
+        constexpr int JT = D == 256 ? 2 : 3;
+        const auto kernel = lora_stream_kernel<T, D, JT, false>;
+        const int smem = StreamLds<T, D, 1>::bytes(a.rank8);
+        if (const int e = allow_lds(kernel, smem); e != hipSuccess) return e;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((rows + ROWS - 1) / ROWS)), dim3(256), smem, s, a);
     }
     return hipGetLastError();
 }
