@@ -2,8 +2,8 @@
 // many circuits at once, each with its own adapter or none.
 //
 //  lora_pack_kernel      lays W, D_a and U_a out once in matrix-core operand order.
-//  lora_stream_kernel    a tile of 32 rows goes to LDS, T = gain (S D_a) for every row by its own adapter, then the output
-//                        columns, first T U_a, then S W on top in the same accumulators, W streaming from the L2: fp32, and
+//  lora_stream_kernel    a tile of 32 rows goes to LDS, the output columns take S W, streaming from the L2, then T U_a on
+//                        top in the same accumulators, with T = gain (S D_a) for every row by its own adapter: fp32, and
 //                        calls with few rows.
 //  lora_resident_kernel  the same with W in registers and a workgroup walking over tiles of 64 rows, half of its waves
 //                        fetching rows and forming T ahead of the others: bfloat16, many rows.
@@ -173,9 +173,9 @@ struct Adapters {
     }
 };
 
-// T U_a for JT column tiles from `tile` on, into zeroed accumulators, two chunks of ranks at a time. A tile of rows with one
-// adapter has its first two chunks requested ahead, by first(). Otherwise adapter after adapter, a column tile at a time, the
-// next two chunks (of the same adapter or the next) requested before these are multiplied.
+// T U_a for JT column tiles from `tile` on, on top of S W in the accumulators, two chunks of ranks at a time. A tile of rows with
+// one adapter has its first two chunks requested ahead, by first(). Otherwise adapter after adapter, a column tile at a time, the
+// next two chunks (of the same adapter or the next) requested before these are multiplied; the sums are kept for its own rows.
 template <typename T, int D, int JT> struct UpProduct {
     uint4 up[2][JT];
     template <int N>
@@ -227,9 +227,7 @@ template <typename T, int D, int JT> struct UpProduct {
             todo &= ~__ballot(ad.mine == a);
             uint4 now[2][1], next[2][1];
             fetch(p, a, 0, tile + j, n, hi, now);
-            f32x16 part;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) part[i] = 0.f;
+            f32x16 part = acc[j];                 // (S W for the rows whose turn has not come; the others are not kept again)
             for (int c0 = 0;;) {
                 const bool ends = c0 + 2 >= chunks, more = !ends || todo != 0;
                 const int a_next = ends && todo ? __builtin_amdgcn_readlane(ad.mine, (int)__builtin_ctzll(todo)) : a;
@@ -239,7 +237,8 @@ template <typename T, int D, int JT> struct UpProduct {
                     if (c0 + c < chunks) Mma<T>::run(now[c][0], low_operand(p, low, c0 + c, n, hi), part);
                 if (ends) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) { acc[j][i] = ad.mine == a ? part[i] : acc[j][i]; part[i] = 0.f; }
+                    for (int i = 0; i < 16; ++i) acc[j][i] = ad.mine == a ? part[i] : acc[j][i];
+                    part = acc[j];
                 }
                 if (!more) break;
                 now[0][0] = next[0][0]; now[1][0] = next[1][0];
@@ -265,9 +264,9 @@ struct Outputs {
 };
 
 // JT finished column tiles of the wave's rows, through its own corner of LDS (a wave's LDS operations complete in order), as
-// 16-byte pieces of rows to Q, K or V
+// 16-byte pieces of rows to Q, K or V; rows without their bit in `leave` stay
 template <typename T, int D, int JT, int STRIDE>
-__device__ __forceinline__ void put_tiles(const Outputs& to, const f32x16* acc, T* out_rows, int64_t r0, int64_t r_end, int tile, int lane)
+__device__ __forceinline__ void put_tiles(const Outputs& to, const f32x16* acc, T* out_rows, int64_t r0, int64_t r_end, int tile, int lane, uint32_t leave)
 {
     constexpr int E = PIECE<T>, PPR = JT * 32 / E;             // pieces per row
     const int n = lane & 31, hi = lane >> 5;
@@ -288,10 +287,14 @@ __device__ __forceinline__ void put_tiles(const Outputs& to, const f32x16* acc, 
     uint4 v[PIECES];
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) v[i] = *((const uint4*)(out_rows + (lane + 64 * i) / PPR * STRIDE) + (lane + 64 * i) % PPR);
+    const int rows = (int)min((int64_t)ROWS, r_end - r0);
+    T* at = to.at<T, D>(r0 + lane / PPR, tile * 32 + lane % PPR * E);
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-        const int piece = lane + 64 * i, row = piece / PPR, cc = piece % PPR;
-        if (r0 + row < r_end) store_stream(to.at<T, D>(r0 + row, tile * 32 + cc * E), v[i]);
+        const int piece = lane + 64 * i, row = piece / PPR;
+        if (64 % PPR != 0 && i > 0) at = to.at<T, D>(r0 + row, tile * 32 + piece % PPR * E);
+        if (row < rows && (leave >> row & 1)) store_stream(at, v[i]);
+        at += 64 / PPR * D;
     }
 }
 
@@ -364,21 +367,6 @@ __global__ __launch_bounds__(256, 2) void lora_stream_kernel(dg4_lora_args p)
         *((uint4*)(rows + (piece / CPR) * L::S_STRIDE) + piece % CPR) = row_piece[i];
     }
     __syncthreads();
-    if (ad.any) {
-        for (int q0 = wave / 2 * 16; ad16.any && q0 < p.rank; q0 += 32) {
-            const T* mine = rows + half * 16 * L::S_STRIDE;
-            f32x4 sum;
-            if (ad16.one) {
-                if (q0 >= 32) fetch_down<T, D>(p, ad16.first, q0, lane, d);
-                sum = down_product<T, D>(d, mine, L::S_STRIDE, lane);
-            } else {
-                sum = down_product_mixed<T, D>(p, ad16.mine, q0, mine, L::S_STRIDE, lane);
-            }
-            // (rows without an adapter get, or have, what is kept for no row)
-            put_low<T>(low + (half * 16 + lane % 16) * low_stride<T>(p.rank8), q0 + lane / 16 * 4, p.rank, p.rank8, sum, gain);
-        }
-        __syncthreads();
-    }
     const Outputs outputs(p);
     auto row_operand = [&](int c) __attribute__((always_inline)) { return *(const uint4*)(rows + n * L::S_STRIDE + (2 * c + hi) * E); };
     // (unrolled, so that the weights on their way are waited for one by one and not behind the stores of a pass)
@@ -390,11 +378,6 @@ __global__ __launch_bounds__(256, 2) void lora_stream_kernel(dg4_lora_args p)
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[j][i] = 0.f;
         const int tile = tile0 + pass * JT;
-        if (ad.any) {
-            if (ad.one) up.run_one(p, ad, low, tile, n, hi, acc);
-            else up.run_mixed(p, ad, low, tile, n, hi, acc);
-        }
-        if (pass + 1 < PASSES) up.first(p, ad, tile + JT, n, hi);
         uint4 b[2];                               // rows as operand: this chunk's and the next's
         b[0] = row_operand(0);
 #pragma unroll
@@ -409,8 +392,28 @@ __global__ __launch_bounds__(256, 2) void lora_stream_kernel(dg4_lora_args p)
             }
             __builtin_amdgcn_sched_barrier(0);
         }
+        if (ad.any) {
+            if (pass == 0) {                      // (T is needed from here on; its D_a has travelled under the first pass)
+                for (int q0 = wave / 2 * 16; ad16.any && q0 < p.rank; q0 += 32) {
+                    const T* mine = rows + half * 16 * L::S_STRIDE;
+                    f32x4 sum;
+                    if (ad16.one) {
+                        if (q0 >= 32) fetch_down<T, D>(p, ad16.first, q0, lane, d);
+                        sum = down_product<T, D>(d, mine, L::S_STRIDE, lane);
+                    } else {
+                        sum = down_product_mixed<T, D>(p, ad16.mine, q0, mine, L::S_STRIDE, lane);
+                    }
+                    // (rows without an adapter get, or have, what is kept for no row)
+                    put_low<T>(low + (half * 16 + lane % 16) * low_stride<T>(p.rank8), q0 + lane / 16 * 4, p.rank, p.rank8, sum, gain);
+                }
+                __syncthreads();
+            }
+            if (ad.one) up.run_one(p, ad, low, tile, n, hi, acc);
+            else up.run_mixed(p, ad, low, tile, n, hi, acc);
+        }
+        if (pass + 1 < PASSES) up.first(p, ad, tile + JT, n, hi);
 #pragma unroll
-        for (int j = 0; j < JT; j += TILES_OUT) put_tiles<T, D, TILES_OUT, L::O_STRIDE>(outputs, acc + j, out_rows, r0, r_end, tile + j, lane);
+        for (int j = 0; j < JT; j += TILES_OUT) put_tiles<T, D, TILES_OUT, L::O_STRIDE>(outputs, acc + j, out_rows, r0, r_end, tile + j, lane, ~0u);
     }
 }
 
@@ -545,60 +548,85 @@ __global__ __launch_bounds__(512, 2) void lora_resident_kernel(dg4_lora_args p)
     T* const out_rows = (T*)(smem + L::out_at(p.rank8)) + wave * ROWS * L::O_STRIDE;
     __syncthreads();
     for (int64_t step = 0; step < steps; ++step) {
-        const int64_t tile_r0 = p.row_begin + (walk + step * walks) * L::TILE;
+        // (a lane number of its own in every step: what is worked out from it is not kept over the loop, where W has the registers)
+        int lane = (int)threadIdx.x & 63;
+        __asm__ volatile("" : "+v"(lane));
+        const int n = lane & 31, hi = lane >> 5;
+        const T* rows = rows_of(step) + n * L::S_STRIDE + hi * E;
+        const T* low = low_of(step);
+        constexpr int H = L::TILE / ROWS;         // halves of the tile, multiplied together
+        constexpr int WINDOW = 2;                 // rows as operand: this chunk's and the next's
+        uint4 b[WINDOW][H];
+        auto fetch_rows = [&](int c) __attribute__((always_inline)) {
+#pragma unroll
+            for (int t = 0; t < H; ++t) b[c % WINDOW][t] = *(const uint4*)(rows + t * ROWS * L::S_STRIDE + 2 * c * E);
+        };
+        auto low_piece = [&](int c, int t) __attribute__((always_inline)) { return UpProduct<T, D, JT>::low_operand(p, low + t * ROWS * low_stride<T>(p.rank8), c, n, hi); };
+        const int64_t r0 = p.row_begin + (walk + step * walks) * L::TILE;
+        int id[H];
+#pragma unroll
+        for (int t = 0; t < H; ++t) id[t] = ids_of(step)[t * ROWS + n];
+        // Once, if all rows have one adapter; else once for every adapter among them, its own rows leaving
+        uint64_t left[H];                         // rows that have not left (a bit per lane: every row twice)
+#pragma unroll
+        for (int t = 0; t < H; ++t) left[t] = ~0ull;
 #pragma unroll 1
-        for (int t = 0; t < L::TILE / ROWS; ++t) {
-            const int64_t r0 = tile_r0 + t * ROWS, r_end = min(p.row_end, r0 + ROWS);
-            if (r0 >= r_end) break;
-            const T* rows = rows_of(step) + t * ROWS * L::S_STRIDE;
-            const T* low = low_of(step) + t * ROWS * low_stride<T>(p.rank8);
-            Adapters ad;
-            ad.set(ids_of(step)[t * ROWS + n], p.n_adapters);
-            f32x16 acc[JT];
+        do {
+            fetch_rows(0);
+            f32x16 acc[H][JT];
 #pragma unroll
-            for (int j = 0; j < JT; ++j)
+            for (int c = 0; c < KC; ++c) {
+                if (c + WINDOW - 1 < KC) fetch_rows(c + WINDOW - 1);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) acc[j][i] = 0.f;
-            if (ad.any && !ad.one) {
-                UpProduct<T, D, JT>::run_mixed(p, ad, low, tile0, n, hi, acc);
-            } else if (ad.any) {
-                if (ad.first != held) {           // (32 lanes a column tile: either half of the wave multiplies the same rows of U_a)
-                    held = ad.first;
+                for (int j = 0; j < JT; ++j)
+#pragma unroll
+                    for (int t = 0; t < H; ++t) {
+                        if (c == 0) {
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) acc[t][j][i] = 0.f;
+                        }
+                        Mma<T>::run(w[j][c], b[c % WINDOW][t], acc[t][j]);
+                    }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            const int a = left[0] ? __builtin_amdgcn_readlane(id[0], (int)__builtin_ctzll(left[0])) : __builtin_amdgcn_readlane(id[H - 1], (int)__builtin_ctzll(left[H - 1]));
+            uint64_t leave[H];
+#pragma unroll
+            for (int t = 0; t < H; ++t) { leave[t] = __ballot(id[t] == a); left[t] &= ~leave[t]; }
+            if (a >= 0) {
+                if (a != held) {                  // (32 lanes a column tile: either half of the wave multiplies the same rows of U_a)
+                    held = a;
                     for (int c = hi; c < chunks; c += 2)
 #pragma unroll
                         for (int j = 0; j < JT; ++j)
                             up_held[(c * JT + j) * 32 + n] = ((const uint4*)p.up_packed)[((int64_t)held * chunks + c) * (3 * D) + (tile0 + j) * 32 + column_of(n)];
                 }
                 for (int c0 = 0; c0 < chunks; c0 += 2) {
-                    uint4 low_piece[2], up_piece[2][JT];
+                    uint4 x[2][H], y[2][JT];
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
                         const int at = min(c0 + c, chunks - 1);
-                        low_piece[c] = UpProduct<T, D, JT>::low_operand(p, low, at, n, hi);
 #pragma unroll
-                        for (int j = 0; j < JT; ++j) up_piece[c][j] = up_held[(at * JT + j) * 32 + n];
+                        for (int t = 0; t < H; ++t) x[c][t] = low_piece(at, t);
+#pragma unroll
+                        for (int j = 0; j < JT; ++j) y[c][j] = up_held[(at * JT + j) * 32 + n];
                     }
 #pragma unroll
-                    for (int c = 0; c < 2; ++c)
+                    for (int c = 0; c < 2; ++c) {
                         if (c0 + c < chunks) {
 #pragma unroll
-                            for (int j = 0; j < JT; ++j) Mma<T>::run(up_piece[c][j], low_piece[c], acc[j]);
+                            for (int j = 0; j < JT; ++j)
+#pragma unroll
+                                for (int t = 0; t < H; ++t) Mma<T>::run(y[c][j], x[c][t], acc[t][j]);
                         }
+                    }
                 }
             }
-            constexpr int WINDOW = 4;             // rows as operand: this chunk's and the next three's
-            uint4 b[WINDOW];
+            __asm__ volatile("" : "+v"(lane));
 #pragma unroll
-            for (int c = 0; c < WINDOW - 1; ++c) b[c] = *(const uint4*)(rows + n * L::S_STRIDE + (2 * c + hi) * E);
-#pragma unroll
-            for (int c = 0; c < KC; ++c) {
-                if (c + WINDOW - 1 < KC) b[(c + WINDOW - 1) % WINDOW] = *(const uint4*)(rows + n * L::S_STRIDE + (2 * (c + WINDOW - 1) + hi) * E);
-#pragma unroll
-                for (int j = 0; j < JT; ++j) Mma<T>::run(w[j][c], b[c % WINDOW], acc[j]);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            put_tiles<T, D, JT, L::O_STRIDE>(outputs, acc, out_rows, r0, r_end, tile0, lane);
-        }
+            for (int t = 0; t < H; ++t)
+                put_tiles<T, D, JT, L::O_STRIDE>(outputs, acc[t], out_rows, r0 + t * ROWS, p.row_end, tile0, lane, (uint32_t)leave[t]);
+        } while (left[0] | left[H - 1]);
         __syncthreads();
     }
 }
