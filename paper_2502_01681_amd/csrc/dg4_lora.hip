@@ -34,13 +34,17 @@ __device__ __forceinline__ void store_stream(void* p, const uint4& v)
 // row; with column 16 hi + 4 a + b at operand row 8 a + 4 hi + b they are 16 neighbouring columns.
 __device__ __forceinline__ int column_of(int m) { return 16 * ((m >> 2) & 1) + 4 * (m >> 3) + (m & 3); }
 
-// Calls of up to so many rows split the columns over workgroups
-constexpr int64_t SPREAD_ROWS = 4096;
+// Calls with up to so many elements of S split the columns over workgroups. Measured, split | not split, in us, rank 16:
+// bfloat16 at hidden 256, 4000 rows 8.8 | 9.9, 8000 rows 12.7 | 13.5, 10,000 rows 15.8 | 14.0; at 128, 4000 rows 5.5 | 9.7,
+// 14,000 rows 8.9 | 9.8; fp32 at 256, 4000 rows 28.9 | 43.9, 12,000 rows 61.8 | 65.0, 20,000 rows 96.5 | 93.9; at 128, 4000 rows
+// 11.7 | 15.0, 20,000 rows 29.6 | 31.4, 40,000 rows 52.0 | 49.7.
+template <typename T> constexpr int64_t SPREAD_ELEMENTS = sizeof(T) == 2 ? 1 << 21 : 1 << 22;
 template <typename T> constexpr int PIECE = 16 / (int)sizeof(T);      // elements of 16 bytes
 inline int rank8(int rank) { return (rank + 7) / 8 * 8; }
 
-// W: unit (tile * KC + c) * 64 + lane holds rows k = (2c + lane/32) E .. + E-1 of column 32 tile + column_of(lane % 32). Down: per adapter, unit (k/E) * rank + n holds rows k .. k+E-1 of column n. Up: per adapter, unit
-// (q/E) * 3D + column holds rows q .. q+E-1, zero from `rank` on (up to the next multiple of eight).
+// W: unit (tile * KC + c) * 64 + lane holds rows k = (2c + lane/32) E .. + E-1 of column 32 tile + column_of(lane % 32).
+// Down: per adapter, unit (k/E) * rank + n holds rows k .. k+E-1 of column n. Up: per adapter, unit (q/E) * 3D + column holds rows
+// q .. q+E-1, zero from `rank` on (up to the next multiple of eight).
 template <typename T, int D>
 __global__ void lora_pack_kernel(dg4_lora_pack_args p)
 {
@@ -651,7 +655,7 @@ template <typename T, int D>
 int launch_proj(dg4_lora_args a, hipStream_t s)
 {
     const int64_t rows = a.row_end - a.row_begin;
-    if (rows <= SPREAD_ROWS) {
+    if (rows * D <= SPREAD_ELEMENTS<T>) {
         const auto kernel = lora_stream_kernel<T, D, 1, true>;
         // rows per tile: few enough for two workgroups per compute unit
         a.tile_rows = 1;

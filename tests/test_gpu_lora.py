@@ -69,7 +69,8 @@ def arrangement(kind, rows, n, rng):
 @pytest.mark.parametrize("hidden", [128, 256])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("rank", [1, 4, 8, 16, 27, 33, 64])
-@pytest.mark.parametrize("kind,rows", [("one", 1), ("own", 64), ("any", 3), ("runs", 131), ("any", 700), ("runs", 4500), ("any", 4500), ("one", 5003)])
+@pytest.mark.parametrize("kind,rows", [("one", 1), ("own", 64), ("any", 3), ("runs", 131), ("any", 700), ("runs", 4500), ("any", 4500), ("one", 5003), ("runs", 17_003),
+                                       ("any", 16_500), ("runs", 33_100)])
 def test_projection(hidden, dtype, rank, kind, rows):
     n = 9 if kind != "own" else 64
     print(f"lora {dtype} {hidden} rank={rank} {kind} rows={rows}", flush=True)
@@ -85,15 +86,17 @@ def test_projection(hidden, dtype, rank, kind, rows):
 
 
 @pytest.mark.parametrize("hidden,dtype,rank", [(128, "f32", 8), (256, "f32", 27), (128, "bf16", 64), (256, "bf16", 16)])
-def test_a_row_depends_on_itself_alone(hidden, dtype, rank):
+@pytest.mark.parametrize("rows", [6011, 33_011])
+def test_a_row_depends_on_itself_alone(hidden, dtype, rank, rows):
     """The same bits in any range of rows, in any order, beside any other adapters; other rows stay."""
-    n, rows = 7, 6011
+    n = 7
     cfg = dg4.LayerConfig(hidden, hidden // 32, 2, 1, dtype)
     W, down, up, gain = weights(3, hidden, n, rank, dtype)
     S, adapter = rows_of(4, rows, hidden, dtype), arrangement("runs", rows, n, np.random.default_rng(2))
     packed = dg4.dg4_lora_pack(cfg, W, down, up, gain)
     whole = project(cfg, packed, S, adapter)
-    for lo, hi in ((0, 1), (1, 3), (5, 38), (100, 612), (63, 4200), (6010, 6011), (17, 17), (1, 6011)):
+    for lo, hi in ((0, 1), (1, 3), (5, 38), (100, 612), (63, 4200), (6010, 6011), (17, 17), (1, 6011), (rows - 17_000, rows - 1), (1, rows)):
+        lo = max(lo, 0)
         part = project(cfg, packed, S, adapter, row_begin=lo, row_end=hi)
         for x, y in zip(part, whole):
             assert torch.equal(x[lo:hi], y[lo:hi]) and (x[:lo] == 7.0).all() and (x[hi:] == 7.0).all(), (lo, hi)
@@ -119,7 +122,7 @@ def test_a_row_depends_on_itself_alone(hidden, dtype, rank):
 
 
 @pytest.mark.parametrize("hidden,dtype", [(128, "f32"), (256, "f32"), (128, "bf16"), (256, "bf16")])
-@pytest.mark.parametrize("rows", [50, 5000])
+@pytest.mark.parametrize("rows", [50, 5000, 33_000])
 def test_without_adapters(hidden, dtype, rows):
     cfg = dg4.LayerConfig(hidden, hidden // 32, 2, 1, dtype)
     W, down, up, gain = weights(3, hidden, 2, 8, dtype)
@@ -210,7 +213,7 @@ def test_serving_path(hidden, dtype, fmt):
 def test_two_graphs_and_a_stream_share_the_packed_weights():
     cfg = dg4.LayerConfig(256, 8, 2, 1, "bf16")
     packed = dg4.dg4_lora_pack(cfg, *weights(1, 256, 4, 16, "bf16"))
-    cases = [(rows_of(s, rows, 256, "bf16"), arrangement("any", rows, 4, np.random.default_rng(s))) for s, rows in ((1, 300), (2, 5000))]
+    cases = [(rows_of(s, rows, 256, "bf16"), arrangement("any", rows, 4, np.random.default_rng(s))) for s, rows in ((1, 300), (2, 9000))]
     want = [project(cfg, packed, *c) for c in cases]
     outs = [[torch.zeros_like(c[0]) for _ in range(3)] for c in cases]
     graphs = []
