@@ -79,7 +79,6 @@ template <> struct Eight<float> {
     uint4 a, b;
     __device__ void load(const float* p) { a = ((const uint4*)p)[0]; b = ((const uint4*)p)[1]; }
     __device__ void get(float* f) const { Elem<float>::unpack(a, b, f); }
-    __device__ static void put(const float* f, float* p) { uint4 a, b; Elem<float>::pack(f, a, b); ((uint4*)p)[0] = a; ((uint4*)p)[1] = b; }
 };
 template <> struct Eight<bf16_t> {
     uint4 a;
@@ -90,14 +89,13 @@ template <> struct Eight<bf16_t> {
 #pragma unroll
         for (int i = 0; i < 4; ++i) { f[2 * i] = bf16_lo(w[i]); f[2 * i + 1] = bf16_hi(w[i]); }
     }
-    __device__ static void put(const float* f, bf16_t* p)
-    {
-        *(uint4*)p = make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
-    }
 };
 
 // A lane takes eight features, so a head is four lanes and a gate's K | V row a whole wave at hidden 256 (two gates at
-// 128): one 512-byte (256-byte) row of codes per store instruction. U gates per lane, all requested before the first is used.
+// 128): one 512-byte (256-byte) row of codes per store instruction. U gates per lane, all requested before the first is used;
+// with two there are enough loads on their way for the whole card and enough workgroups for a level: 1, 2 and 4 gates per lane
+// take 259, 256 and 269 us for a million rows of bfloat16 at hidden 256 (1.56 GB moved, 6.1 TB/s) and 3.1, 3.3 and 3.9 us for
+// 264. Codes leave through the caches, where the next level's attention finds them (past them: 249 us).
 template <typename T, int FMT, int D, int U>
 __global__ __launch_bounds__(256) void kv8_write_kernel(dg4_kv8_args p)
 {
@@ -142,17 +140,28 @@ __global__ __launch_bounds__(256) void kv8_write_kernel(dg4_kv8_args p)
     }
 }
 
+// Results leave past the caches
+__device__ __forceinline__ void store_stream(void* p, const uint4& v)
+{
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), (u32x4*)p);
+}
+
+// A lane takes what it stores as 16 bytes, so that a wave's store is whole lines: four features of fp32, eight of bfloat16
+// (402,193 rows of fp32 at hidden 256, 1.04 GB moved: 250 us with two 16-byte stores a lane, of every other piece each, 155 us, 6.7
+// TB/s, so; 181 us where rows leave through the caches). U rows per lane: 185, 155 and 175 us with 1, 2 and 4.
 template <typename T, int FMT, int D, int U>
 __global__ __launch_bounds__(256) void kv8_read_kernel(dg4_kv8_args p)
 {
-    constexpr int LPG = 2 * D / 8;
+    constexpr int PER = 16 / (int)sizeof(T);
+    constexpr int LPG = 2 * D / PER;
     constexpr int GPB = 256 / LPG;
     const int sub = (int)threadIdx.x % LPG;
     const int64_t r0 = p.row_begin + (int64_t)blockIdx.x * (GPB * U) + (int)threadIdx.x / LPG;
     const bool is_v = sub >= LPG / 2;
-    const int col = (sub % (LPG / 2)) * 8;
+    const int col = (sub % (LPG / 2)) * PER;
     T* dst = (T*)(is_v ? p.v_out : p.k_out) + col;
-    uint2 w[U];
+    uint32_t w[U][PER / 4];
     uint32_t byte[U];
     bool in[U];
 #pragma unroll
@@ -163,28 +172,31 @@ __global__ __launch_bounds__(256) void kv8_read_kernel(dg4_kv8_args p)
         if (in[u]) at = p.ids ? (int64_t)p.ids[r] : r;
         in[u] = in[u] && at >= 0 && at < p.n_store;
         if (!in[u]) at = 0;                                   // (the store has a row: the launcher checks)
-        w[u] = *(const uint2*)(p.codes + at * (2 * D) + sub * 8);
-        byte[u] = p.scales[at * (2 * D / 32) + (sub % (LPG / 2)) / 4 * 2 + (is_v ? 1 : 0)];
+        const uint8_t* from = p.codes + at * (2 * D) + sub * PER;
+        if constexpr (PER == 8) {
+            const uint2 two = *(const uint2*)from;
+            w[u][0] = two.x; w[u][1] = two.y;
+        } else {
+            w[u][0] = *(const uint32_t*)from;
+        }
+        byte[u] = p.scales[at * (2 * D / 32) + col / 32 * 2 + (is_v ? 1 : 0)];
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        float f[8];
-        decode4<FMT>(w[u].x, f); decode4<FMT>(w[u].y, f + 4);
+        float f[PER];
+#pragma unroll
+        for (int i = 0; i < PER / 4; ++i) decode4<FMT>(w[u][i], f + 4 * i);
         const float scale = scale_value(byte[u]);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] *= scale;
-        if (in[u]) Eight<T>::put(f, dst + (r0 + (int64_t)u * GPB) * D);
+        for (int i = 0; i < PER; ++i) f[i] *= scale;
+        uint4 out;
+        if constexpr (PER == 8) out = make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
+        else out = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+        if (in[u]) store_stream(dst + (r0 + (int64_t)u * GPB) * D, out);
     }
 }
 
 // ------------------------------------------------------------------------------------------------- attention
-
-// Results leave past the caches, which are the store's (1 to 7 % of the time)
-__device__ __forceinline__ void store_stream(void* p, const uint4& v)
-{
-    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-    __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), (u32x4*)p);
-}
 
 // What an entry that is none reads where buffer addressing does not reach (FAR, below)
 __device__ __align__(256) const uint8_t nothing[512] = {};
@@ -406,17 +418,18 @@ int launch_write(const dg4_kv8_args& a, hipStream_t s)
 {
     constexpr int GPB = 256 / (2 * D / 8);
     const int64_t rows = a.row_end - a.row_begin;
-    const unsigned grid = (unsigned)((rows + GPB * 4 - 1) / (GPB * 4));
-    hipLaunchKernelGGL((kv8_write_kernel<T, FMT, D, 4>), dim3(grid), dim3(256), 0, s, a);
+    const unsigned grid = (unsigned)((rows + GPB * 2 - 1) / (GPB * 2));
+    hipLaunchKernelGGL((kv8_write_kernel<T, FMT, D, 2>), dim3(grid), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 template <typename T, int FMT, int D>
 int launch_read(const dg4_kv8_args& a, hipStream_t s)
 {
-    constexpr int GPB = 256 / (2 * D / 8);
+    constexpr int GPB = 256 / (2 * D / (16 / (int)sizeof(T)));
+    constexpr int U = 2;
     const int64_t rows = a.row_end - a.row_begin;
-    const unsigned grid = (unsigned)((rows + GPB * 4 - 1) / (GPB * 4));
-    hipLaunchKernelGGL((kv8_read_kernel<T, FMT, D, 4>), dim3(grid), dim3(256), 0, s, a);
+    const unsigned grid = (unsigned)((rows + GPB * U - 1) / (GPB * U));
+    hipLaunchKernelGGL((kv8_read_kernel<T, FMT, D, U>), dim3(grid), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 // The split goes by the table's width alone, so a row's result does not depend on which rows a call covers.
