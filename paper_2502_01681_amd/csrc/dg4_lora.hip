@@ -452,8 +452,9 @@ __global__ __launch_bounds__(512, 2) void lora_resident_kernel(dg4_lora_args p)
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 31, hi = lane >> 5;
     // workgroups go to the eight XCDs in turn
-    const int xcd = (int)blockIdx.x & 7, slot = (int)blockIdx.x >> 3, walks = (int)(gridDim.x / (8 * PARTS)) * 8;
-    const int share = slot % PARTS, walk = slot / PARTS * 8 + xcd;
+    const int walks = (int)gridDim.x / PARTS, whole = walks / 8 * (8 * PARTS);     // (those of the walks left over by eight go apart)
+    const int xcd = (int)blockIdx.x & 7, slot = (int)blockIdx.x >> 3, over = (int)blockIdx.x - whole;
+    const int share = (over < 0 ? slot : over) % PARTS, walk = over < 0 ? slot / PARTS * 8 + xcd : (whole + over) / PARTS;
     const int64_t tiles = (p.row_end - p.row_begin + L::TILE - 1) / L::TILE;
     const int64_t steps = walk < tiles ? (tiles - walk + walks - 1) / walks : 0;   // tiles walk, walk + walks, ...
     if (steps == 0) return;
@@ -671,9 +672,9 @@ int launch_proj(dg4_lora_args a, hipStream_t s)
         if (const int e = allow_lds(kernel, smem); e != hipSuccess) return e;
         int dev = 0, cus = 0;
         if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess) return hipErrorInvalidDevice;
-        // one workgroup per compute unit, as whole walks on every XCD
-        const int64_t walks = std::max<int64_t>(1, std::min<int64_t>(cus / (8 * PARTS), ((rows + L::TILE - 1) / L::TILE + 7) / 8));
-        hipLaunchKernelGGL(kernel, dim3((unsigned)(8 * PARTS * walks)), dim3(512), smem, s, a);
+        // one workgroup per compute unit
+        const int64_t walks = std::min<int64_t>(std::max(1, cus / PARTS), (rows + L::TILE - 1) / L::TILE);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)(PARTS * walks)), dim3(512), smem, s, a);
     } else {
         constexpr int JT = D == 256 ? 2 : 3;
         const auto kernel = lora_stream_kernel<T, D, JT, false>;
