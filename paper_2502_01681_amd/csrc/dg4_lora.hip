@@ -268,9 +268,9 @@ struct Outputs {
 };
 
 // JT finished column tiles of the wave's rows, through its own corner of LDS (a wave's LDS operations complete in order), as
-// 16-byte pieces of rows to Q, K or V; rows without their bit in `leave` stay
+// 16-byte pieces of rows to Q, K or V
 template <typename T, int D, int JT, int STRIDE>
-__device__ __forceinline__ void put_tiles(const Outputs& to, const f32x16* acc, T* out_rows, int64_t r0, int64_t r_end, int tile, int lane, uint32_t leave)
+__device__ __forceinline__ void put_tiles(const Outputs& to, const f32x16* acc, T* out_rows, int64_t r0, int64_t r_end, int tile, int lane)
 {
     constexpr int E = PIECE<T>, PPR = JT * 32 / E;             // pieces per row
     const int n = lane & 31, hi = lane >> 5;
@@ -297,7 +297,7 @@ __device__ __forceinline__ void put_tiles(const Outputs& to, const f32x16* acc, 
     for (int i = 0; i < PIECES; ++i) {
         const int piece = lane + 64 * i, row = piece / PPR;
         if (64 % PPR != 0 && i > 0) at = to.at<T, D>(r0 + row, tile * 32 + piece % PPR * E);
-        if (row < rows && (leave >> row & 1)) store_stream(at, v[i]);
+        if (row < rows) store_stream(at, v[i]);
         at += 64 / PPR * D;
     }
 }
@@ -417,7 +417,7 @@ __global__ __launch_bounds__(256, 2) void lora_stream_kernel(dg4_lora_args p)
         }
         if (pass + 1 < PASSES) up.first(p, ad, tile + JT, n, hi);
 #pragma unroll
-        for (int j = 0; j < JT; j += TILES_OUT) put_tiles<T, D, TILES_OUT, L::O_STRIDE>(outputs, acc + j, out_rows, r0, r_end, tile + j, lane, ~0u);
+        for (int j = 0; j < JT; j += TILES_OUT) put_tiles<T, D, TILES_OUT, L::O_STRIDE>(outputs, acc + j, out_rows, r0, r_end, tile + j, lane);
     }
 }
 
@@ -559,33 +559,24 @@ __global__ __launch_bounds__(512, 2) void lora_resident_kernel(dg4_lora_args p)
         const int n = lane & 31, hi = lane >> 5;
         const T* rows = rows_of(step) + n * L::S_STRIDE + hi * E;
         const T* low = low_of(step);
-        constexpr int H = L::TILE / ROWS;         // halves of the tile, multiplied together
+        constexpr int H = L::TILE / ROWS;         // halves of the tile, multiplied together if all rows have one adapter
         constexpr int WINDOW = 2;                 // rows as operand: this chunk's and the next's
-        uint4 b[WINDOW][H];
-        auto fetch_rows = [&](int c) __attribute__((always_inline)) {
+        // COUNT halves from `t0` on times W
+        auto multiply = [&](auto count, int t0, f32x16 (*acc)[JT]) __attribute__((always_inline)) {
+            constexpr int COUNT = count;
+            uint4 b[WINDOW][COUNT];
+            auto fetch_rows = [&](int c) __attribute__((always_inline)) {
 #pragma unroll
-            for (int t = 0; t < H; ++t) b[c % WINDOW][t] = *(const uint4*)(rows + t * ROWS * L::S_STRIDE + 2 * c * E);
-        };
-        auto low_piece = [&](int c, int t) __attribute__((always_inline)) { return UpProduct<T, D, JT>::low_operand(p, low + t * ROWS * low_stride<T>(p.rank8), c, n, hi); };
-        const int64_t r0 = p.row_begin + (walk + step * walks) * L::TILE;
-        int id[H];
-#pragma unroll
-        for (int t = 0; t < H; ++t) id[t] = ids_of(step)[t * ROWS + n];
-        // Once, if all rows have one adapter; else once for every adapter among them, its own rows leaving
-        uint64_t left[H];                         // rows that have not left (a bit per lane: every row twice)
-#pragma unroll
-        for (int t = 0; t < H; ++t) left[t] = ~0ull;
-#pragma unroll 1
-        do {
+                for (int t = 0; t < COUNT; ++t) b[c % WINDOW][t] = *(const uint4*)(rows + (t0 + t) * ROWS * L::S_STRIDE + 2 * c * E);
+            };
             fetch_rows(0);
-            f32x16 acc[H][JT];
 #pragma unroll
             for (int c = 0; c < KC; ++c) {
                 if (c + WINDOW - 1 < KC) fetch_rows(c + WINDOW - 1);
 #pragma unroll
                 for (int j = 0; j < JT; ++j)
 #pragma unroll
-                    for (int t = 0; t < H; ++t) {
+                    for (int t = 0; t < COUNT; ++t) {
                         if (c == 0) {
 #pragma unroll
                             for (int i = 0; i < 16; ++i) acc[t][j][i] = 0.f;
@@ -594,44 +585,74 @@ __global__ __launch_bounds__(512, 2) void lora_resident_kernel(dg4_lora_args p)
                     }
                 __builtin_amdgcn_sched_barrier(0);
             }
-            const int a = left[0] ? __builtin_amdgcn_readlane(id[0], (int)__builtin_ctzll(left[0])) : __builtin_amdgcn_readlane(id[H - 1], (int)__builtin_ctzll(left[H - 1]));
-            uint64_t leave[H];
+        };
+        // T U_a on top for the same halves
+        auto multiply_up = [&](auto count, int t0, int a, f32x16 (*acc)[JT]) __attribute__((always_inline)) {
+            constexpr int COUNT = count;
+            if (a != held) {                      // (32 lanes a column tile: either half of the wave multiplies the same rows of U_a)
+                held = a;
+                for (int c = hi; c < chunks; c += 2)
 #pragma unroll
-            for (int t = 0; t < H; ++t) { leave[t] = __ballot(id[t] == a); left[t] &= ~leave[t]; }
-            if (a >= 0) {
-                if (a != held) {                  // (32 lanes a column tile: either half of the wave multiplies the same rows of U_a)
-                    held = a;
-                    for (int c = hi; c < chunks; c += 2)
+                    for (int j = 0; j < JT; ++j)
+                        up_held[(c * JT + j) * 32 + n] = ((const uint4*)p.up_packed)[((int64_t)held * chunks + c) * (3 * D) + (tile0 + j) * 32 + column_of(n)];
+            }
+            for (int c0 = 0; c0 < chunks; c0 += 2) {
+                uint4 x[2][COUNT], y[2][JT];
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const int at = min(c0 + c, chunks - 1);
+#pragma unroll
+                    for (int t = 0; t < COUNT; ++t) x[c][t] = UpProduct<T, D, JT>::low_operand(p, low + (t0 + t) * ROWS * low_stride<T>(p.rank8), at, n, hi);
+#pragma unroll
+                    for (int j = 0; j < JT; ++j) y[c][j] = up_held[(at * JT + j) * 32 + n];
+                }
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    if (c0 + c < chunks) {
 #pragma unroll
                         for (int j = 0; j < JT; ++j)
-                            up_held[(c * JT + j) * 32 + n] = ((const uint4*)p.up_packed)[((int64_t)held * chunks + c) * (3 * D) + (tile0 + j) * 32 + column_of(n)];
-                }
-                for (int c0 = 0; c0 < chunks; c0 += 2) {
-                    uint4 x[2][H], y[2][JT];
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        const int at = min(c0 + c, chunks - 1);
-#pragma unroll
-                        for (int t = 0; t < H; ++t) x[c][t] = low_piece(at, t);
-#pragma unroll
-                        for (int j = 0; j < JT; ++j) y[c][j] = up_held[(at * JT + j) * 32 + n];
-                    }
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        if (c0 + c < chunks) {
-#pragma unroll
-                            for (int j = 0; j < JT; ++j)
-#pragma unroll
-                                for (int t = 0; t < H; ++t) Mma<T>::run(y[c][j], x[c][t], acc[t][j]);
-                        }
+                            for (int t = 0; t < COUNT; ++t) Mma<T>::run(y[c][j], x[c][t], acc[t][j]);
                     }
                 }
             }
+        };
+        const int64_t r0 = p.row_begin + (walk + step * walks) * L::TILE;
+        int id[H];
+#pragma unroll
+        for (int t = 0; t < H; ++t) id[t] = ids_of(step)[t * ROWS + n];
+        const int first = __builtin_amdgcn_readfirstlane(id[0]);
+        if (__ballot(id[0] != first || id[H - 1] != first) == 0) {
+            f32x16 acc[H][JT];
+            multiply(std::integral_constant<int, H>{}, 0, acc);
+            if (first >= 0) multiply_up(std::integral_constant<int, H>{}, 0, first, acc);
             __asm__ volatile("" : "+v"(lane));
 #pragma unroll
-            for (int t = 0; t < H; ++t)
-                put_tiles<T, D, JT, L::O_STRIDE>(outputs, acc[t], out_rows, r0 + t * ROWS, p.row_end, tile0, lane, (uint32_t)leave[t]);
-        } while (left[0] | left[H - 1]);
+            for (int t = 0; t < H; ++t) put_tiles<T, D, JT, L::O_STRIDE>(outputs, acc[t], out_rows, r0 + t * ROWS, p.row_end, tile0, lane);
+        } else {
+            // Adapter after adapter, on top of S W, kept for its own rows
+#pragma unroll 1
+            for (int t = 0; t < H; ++t) {
+                const int mine = t == 0 ? id[0] : id[H - 1];
+                f32x16 acc[1][JT];
+                multiply(std::integral_constant<int, 1>{}, t, acc);
+                uint64_t todo = __ballot(mine >= 0);
+#pragma unroll 1
+                while (todo) {
+                    const int a = __builtin_amdgcn_readlane(mine, (int)__builtin_ctzll(todo));
+                    todo &= ~__ballot(mine == a);
+                    f32x16 part[1][JT];
+#pragma unroll
+                    for (int j = 0; j < JT; ++j) part[0][j] = acc[0][j];
+                    multiply_up(std::integral_constant<int, 1>{}, t, a, part);
+#pragma unroll
+                    for (int j = 0; j < JT; ++j)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) acc[0][j][i] = mine == a ? part[0][j][i] : acc[0][j][i];
+                }
+                put_tiles<T, D, JT, L::O_STRIDE>(outputs, acc[0], out_rows, r0 + t * ROWS, p.row_end, tile0, lane);
+            }
+        }
         __syncthreads();
     }
 }
