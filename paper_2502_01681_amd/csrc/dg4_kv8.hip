@@ -9,6 +9,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "dg4_device.h"
 #include "dg4_internal.h"
 #include "dg4_rowops.h"
@@ -413,39 +415,44 @@ __global__ __launch_bounds__(256) void kv8_attn_kernel(dg4_kv8_attn_args p)
     }
 }
 
-template <typename T, int FMT, int D>
-int launch_write(const dg4_kv8_args& a, hipStream_t s)
+// launch(args, workgroups) for the rows of a call. A launch holds fewer than 2^32 threads, 2^24 workgroups: longer calls take several.
+template <typename A, typename F> int launch_rows(A a, int rows_per_block, F&& launch)
 {
-    constexpr int GPB = 256 / (2 * D / 8);
-    const int64_t rows = a.row_end - a.row_begin;
-    const unsigned grid = (unsigned)((rows + GPB * 2 - 1) / (GPB * 2));
-    hipLaunchKernelGGL((kv8_write_kernel<T, FMT, D, 2>), dim3(grid), dim3(256), 0, s, a);
-    return hipGetLastError();
+    const int64_t end = a.row_end, most = ((int64_t)1 << 23) * rows_per_block;
+    for (; a.row_begin < end; a.row_begin = a.row_end) {
+        a.row_end = std::min(end, a.row_begin + most);
+        launch(a, dim3((unsigned)((a.row_end - a.row_begin + rows_per_block - 1) / rows_per_block)));
+        if (const int e = hipGetLastError(); e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 template <typename T, int FMT, int D>
-int launch_read(const dg4_kv8_args& a, hipStream_t s)
+int launch_write(const dg4_kv8_args& args, hipStream_t s)
 {
-    constexpr int GPB = 256 / (2 * D / (16 / (int)sizeof(T)));
     constexpr int U = 2;
-    const int64_t rows = a.row_end - a.row_begin;
-    const unsigned grid = (unsigned)((rows + GPB * U - 1) / (GPB * U));
-    hipLaunchKernelGGL((kv8_read_kernel<T, FMT, D, U>), dim3(grid), dim3(256), 0, s, a);
-    return hipGetLastError();
+    return launch_rows(args, 256 / (2 * D / 8) * U, [&](const dg4_kv8_args& a, dim3 grid) {
+        hipLaunchKernelGGL((kv8_write_kernel<T, FMT, D, U>), grid, dim3(256), 0, s, a);
+    });
+}
+template <typename T, int FMT, int D>
+int launch_read(const dg4_kv8_args& args, hipStream_t s)
+{
+    constexpr int U = 2;
+    return launch_rows(args, 256 / (2 * D / (16 / (int)sizeof(T))) * U, [&](const dg4_kv8_args& a, dim3 grid) {
+        hipLaunchKernelGGL((kv8_read_kernel<T, FMT, D, U>), grid, dim3(256), 0, s, a);
+    });
 }
 // The split goes by the table's width alone, so a row's result does not depend on which rows a call covers.
 template <typename T, int FMT, int D, bool FAR>
-int launch_attn_from(const dg4_kv8_attn_args& a, hipStream_t s)
+int launch_attn_from(const dg4_kv8_attn_args& args, hipStream_t s)
 {
     constexpr int GPW = 64 / (D / 16);
-    const int64_t rows = a.row_end - a.row_begin;
-    auto grid = [&](int rows_per_block) { return dim3((unsigned)((rows + rows_per_block - 1) / rows_per_block)); };
-    if (a.ell_w <= 8)
-        hipLaunchKernelGGL((kv8_attn_kernel<T, FMT, D, 2, 4, true, FAR>), grid(4 * GPW / 2), dim3(256), 0, s, a);
-    else if (a.ell_w <= 16)
-        hipLaunchKernelGGL((kv8_attn_kernel<T, FMT, D, 2, 8, true, FAR>), grid(4 * GPW / 2), dim3(256), 0, s, a);
-    else
-        hipLaunchKernelGGL((kv8_attn_kernel<T, FMT, D, GPW, 4, false, FAR>), grid(4), dim3(256), 0, s, a);
-    return hipGetLastError();
+    const bool once = args.ell_w <= 16;
+    return launch_rows(args, once ? 4 * GPW / 2 : 4, [&](const dg4_kv8_attn_args& a, dim3 grid) {
+        if (a.ell_w <= 8) hipLaunchKernelGGL((kv8_attn_kernel<T, FMT, D, 2, 4, true, FAR>), grid, dim3(256), 0, s, a);
+        else if (once) hipLaunchKernelGGL((kv8_attn_kernel<T, FMT, D, 2, 8, true, FAR>), grid, dim3(256), 0, s, a);
+        else hipLaunchKernelGGL((kv8_attn_kernel<T, FMT, D, GPW, 4, false, FAR>), grid, dim3(256), 0, s, a);
+    });
 }
 template <typename T, int FMT, int D>
 int launch_attn(const dg4_kv8_attn_args& a, hipStream_t s)

@@ -356,6 +356,27 @@ def test_captured_and_on_other_streams(hidden, dtype):
         assert all(torch.equal(a, b) for a, b in zip(got, out + [codes, scales])), step
 
 
+def test_more_rows_than_a_launch_holds():
+    c, n, rows = cfg(128, "bf16", 5), 400, 2 ** 26 + 5
+    print(f"kv8 attention over {rows} rows, nearly all padding", flush=True)
+    g = circuit(n, 24, 5)
+    assert np.diff(g.array("nbr_ptr")).max() > 16              # (four rows to a workgroup)
+    codes, scales = store(2, n, 128, "int8")
+    bias = torch.zeros((4, 4), device="cuda")
+    at = torch.tensor([0, 3, 2 ** 25 - 1, 2 ** 25, 2 ** 25 + 6, 2 ** 26 - 1, 2 ** 26, rows - 1], device="cuda")
+    gates = torch.tensor([5, 399, 0, 17, 398, 5, 100, 250], dtype=torch.int32, device="cuda")
+    few = rows_of(1, 8, 128, "bf16")
+    want = torch.zeros_like(few)
+    dg4.dg4_sparse_attn_kv8_fwd(c, "int8", g, few, codes, scales, bias, want, ids=gates)
+    ids = torch.full((rows,), -1, dtype=torch.int32, device="cuda")
+    Q, A = (torch.full((rows, 128), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    ids[at], Q[at] = gates, few
+    dg4.dg4_sparse_attn_kv8_fwd(c, "int8", g, Q, codes, scales, bias, A, ids=ids)
+    assert torch.equal(A[at], want)
+    A[at] = 7.0
+    assert torch.equal(A, A[:1].expand_as(A))
+
+
 def test_binding_checks():
     """Shapes, types, formats and places that do not fit are turned away before anything is queued; nothing to do is fine."""
     n, hidden = 6, 128
