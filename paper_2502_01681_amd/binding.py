@@ -399,7 +399,7 @@ def dg4_lora_pack(cfg: LayerConfig, Wqkv, Down=None, Up=None, gain=None) -> Lora
     if (Down is None) != (Up is None):
         raise DG4Error(-1, where)
     n, rank = (0, 1) if Down is None else (Down.shape[0], Down.shape[-1])
-    if _refused(Wqkv, td, dev, 3 * d * d) or n and (
+    if _refused(Wqkv, td, dev, 3 * d * d) or tuple(Wqkv.shape) != (d, 3 * d) or n and (
             tuple(Down.shape) != (n, d, rank) or tuple(Up.shape) != (n, rank, 3 * d) or _refused(Down, td, dev, n * d * rank) or
             _refused(Up, td, dev, 3 * n * d * rank) or gain is not None and _refused(gain, _types["f32"], dev, n)):
         raise DG4Error(-1, where)
@@ -440,7 +440,7 @@ def _store_call(where: str, cfg: LayerConfig, fmt: str, codes, scales, ids, x, y
     row_end = rows if row_end is None else row_end
     if (fmt not in KV_FORMATS or row_end > rows or _refused(x, td, dev, rows * cfg.hidden) or
             _refused(y, td, dev, rows * cfg.hidden) or _refused(codes, _types["bytes"], dev, n * 2 * cfg.hidden) or
-            _refused(scales, _types["bytes"], dev, n * 2 * cfg.heads) or
+            _refused(scales, _types["bytes"], dev, n * 2 * cfg.heads) or scales.shape != (n, cfg.heads, 2) or
             ids is not None and _refused(ids, _types["ids"], dev, rows)):
         raise DG4Error(-1, where)
     if row_begin == row_end == 0 or n == 0 and ids is not None:      # (an empty tensor has no address)

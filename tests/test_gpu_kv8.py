@@ -387,7 +387,7 @@ def test_binding_checks():
     i = lambda k, t=torch.int32: torch.zeros(k, dtype=t, device="cuda")
     good = dict(x=f(n, hidden), y=f(n, hidden), codes=b(n, 256), scales=b(n, 4, 2), ids=i(n), fmt="int8", cfg=c, bias=f(4, 4))
     bad = [dict(x=f(n, hidden).double()), dict(x=f(n, hidden).cpu()), dict(y=f(n - 1, hidden)), dict(x=f(hidden, n).t()), dict(codes=b(n, 255)),
-           dict(codes=b(n, 256).float()), dict(scales=b(n, 8, 2)), dict(scales=b(n - 1, 4, 2)), dict(ids=i(n - 1)), dict(ids=i(n, torch.int64)),
+           dict(codes=b(n, 256).float()), dict(scales=b(n, 8, 2)), dict(scales=b(n - 1, 4, 2)), dict(scales=b(n, 2, 4)), dict(scales=b(n, 8)), dict(ids=i(n - 1)), dict(ids=i(n, torch.int64)),
            dict(ids=i(n).cpu()), dict(fmt="fp8"), dict(cfg=cfg(hidden, "bf16")), dict(cfg=dg4.LayerConfig(256, 8, 2, 1, "f32")),
            dict(cfg=dg4.LayerConfig(hidden, 4, 2, 1, "f16")), dict(y=f(2 * n, hidden)[::2])]
     attn_only = [dict(bias=f(3, 4)), dict(bias=f(4, 4).double()), dict(cfg=cfg(hidden, "f32", 3))]

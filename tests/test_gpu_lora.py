@@ -243,7 +243,8 @@ def test_binding_checks():
     W, down, up, gain = weights(1, d, n, rank, "bf16")
     for args in ((W[:, :300], down, up, gain), (W.float(), down, up, gain), (W, down, None, gain), (W, down, up[:2], gain), (W, down.float(), up, gain),
                  (W, down, up, gain[:2]), (W, down, up, gain.double()), (W, down.cpu(), up, gain), (W, down.transpose(1, 2), up, gain),
-                 (W.t(), down, up, gain), (W, torch.zeros((n, d, 65), dtype=W.dtype, device="cuda"), torch.zeros((n, 65, 3 * d), dtype=W.dtype, device="cuda"), gain)):
+                 (W.t(), down, up, gain), (W.t().contiguous(), down, up, gain), (W.flatten(), down, up, gain),
+                 (W, torch.zeros((n, d, 65), dtype=W.dtype, device="cuda"), torch.zeros((n, 65, 3 * d), dtype=W.dtype, device="cuda"), gain)):
         with pytest.raises(dg4.DG4Error):
             dg4.dg4_lora_pack(cfg, *args)
     packed = dg4.dg4_lora_pack(cfg, W, down, up, gain)
