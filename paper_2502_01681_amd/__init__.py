@@ -1,6 +1,6 @@
 """dg4: the sparse graph-attention layer of DeepGate4 on MI355X (gfx950).
 
-Thin Python binding over the C ABI in include/dg4.h. Every step of the path
+Thin Python binding over the C ABI in include/dg4.h and include/dg4_serving.h. Every step of the path
 runs in the HIP library; this package only marshals pointers. PyTorch is used
 for device memory and streams.
 """

@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "dg4.h"
+#include "dg4_serving.h"
 
 // Neighbour rows on the device: fixed-width rows of packed 32-bit entries
 // (relation code << 30 | index), padded with DG4_ELL_PAD. Width = 2^(hops+1), at least 8:

@@ -1,5 +1,7 @@
 """What the calls with low-rank adapters turn away, before any device call (pointers here are never dereferenced)."""
 import ctypes
+import os
+import re
 
 import paper_2502_01681_amd as dg4
 
@@ -20,6 +22,14 @@ def pack(c=None, W=P, n=4, rank=8, down=P, up=P, gain=P, packed=P, size=BIG):
 def proj(c=None, packed=P, size=BIG, n=4, rank=8, S=P, lo=0, hi=0, adapter=P, Q=P, K=P, V=P):
     c = (c or cfg()).c()
     return dg4.lib().dg4_qkv_proj_lora(ctypes.byref(c), packed, size, n, rank, S, lo, hi, adapter, Q, K, V, None)
+
+
+def test_library_exports_what_the_header_declares():
+    hdr = open(os.path.join(os.path.dirname(__file__), "..", "include", "dg4_serving.h")).read()
+    names = set(re.findall(r"^(?:int|int64_t)\s+(dg4_[a-z0-9_]+)\s*\(", hdr, flags=re.M))
+    assert names == {"dg4_kv8_write", "dg4_kv8_read", "dg4_sparse_attn_kv8_fwd", "dg4_lora_packed_bytes", "dg4_lora_pack", "dg4_qkv_proj_lora"}
+    for n in names:
+        assert hasattr(dg4.lib(), n) and hasattr(dg4, n), n
 
 
 def test_pack():
