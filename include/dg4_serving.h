@@ -43,7 +43,8 @@ int dg4_kv8_write(const dg4_layer_cfg* cfg, int32_t format, const void* K, const
 /*
  * Rows [row_begin, row_end) of K and V [*, hidden] from the store: row r is store row ids[r] (any
  * number of times the same), or row r without ids. Rows whose id is outside [0, n_store) stay as they
- * are. Exact in float and bfloat16 (a code has at most 8 significant bits) as far as the type reaches.
+ * are. K and V may not overlap (EINVAL). Exact in float and bfloat16 (a code has at most 8 significant
+ * bits) as far as the type reaches.
  */
 int dg4_kv8_read(const dg4_layer_cfg* cfg, int32_t format, const uint8_t* codes, const uint8_t* scales,
                  int64_t n_store, const int32_t* ids /* nullable, device */,
@@ -55,8 +56,9 @@ int dg4_kv8_read(const dg4_layer_cfg* cfg, int32_t format, const uint8_t* codes,
  * [0, n_nodes) stay as they are), or gate r without ids (then row_end <= n_nodes). Scores, softmax and
  * sums in fp32, one rounding to cfg->dtype. rel_bias = -infinity leaves a head's sources of that
  * relation out: what the store holds for them is not looked at, and a head whose sources are all left
- * out gives zeros. The result of a row does not depend on which rows a call covers. The graph's
- * neighbour tables must be on the current device (EINVAL otherwise).
+ * out gives zeros. A may be Q itself, but not overlap it otherwise (EINVAL). The result of a row does
+ * not depend on which rows a call covers. The graph's neighbour tables must be on the current device
+ * (EINVAL otherwise).
  */
 int dg4_sparse_attn_kv8_fwd(const dg4_layer_cfg* cfg, int32_t format, dg4_graph* g,
                             int64_t row_begin, int64_t row_end, const int32_t* ids /* nullable, device */,
@@ -76,9 +78,9 @@ int dg4_sparse_attn_kv8_fwd(const dg4_layer_cfg* cfg, int32_t format, dg4_graph*
  * number of calls and streams at once may share it) for rows [row_begin, row_end) of S; adapter: device
  * int32, one of every row of S, in any order (runs of equal ones cost least); a row whose adapter is
  * outside [0, n_adapters), or any row where adapter is null, gets S[r] Wqkv alone. Q, K, V as in
- * dg4_qkv_proj; they may not alias S. fp32 accumulation, one rounding to cfg->dtype at the end (S Down
- * is carried in at least 16 significant bits in bfloat16). A row's result depends on nothing but the row,
- * its adapter and Wqkv. Allocates nothing, one launch.
+ * dg4_qkv_proj; S, Q, K and V may not overlap (EINVAL). fp32 accumulation, one rounding to cfg->dtype
+ * at the end (S Down is carried in at least 16 significant bits in bfloat16). A row's result depends on
+ * nothing but the row, its adapter and Wqkv. Allocates nothing, one launch.
  */
 #define DG4_MAX_RANK 64
 int64_t dg4_lora_packed_bytes(const dg4_layer_cfg* cfg, int32_t n_adapters, int32_t rank);

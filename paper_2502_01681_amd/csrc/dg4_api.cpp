@@ -154,6 +154,13 @@ SweepEvents& sweep_events() { static SweepEvents e; return e; }
 // rows are read and written as 16-byte pieces
 template <typename... P> bool aligned16(P... ptrs) { return (((uintptr_t)ptrs | ...) & 15) == 0; }
 
+// Whether the same rows of two [*, hidden] tensors share memory
+bool overlap(const dg4_layer_cfg* cfg, const void* a, const void* b, int64_t rows)
+{
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return (x > y ? x - y : y - x) < (uintptr_t)rows * cfg->hidden * (cfg->dtype == DG4_F32 ? 4 : 2);
+}
+
 // What the calls with low-rank adapters share (no adapters: the rank is not looked at)
 int check_lora(const dg4_layer_cfg* cfg, int32_t n_adapters, int32_t* rank)
 {
@@ -374,7 +381,10 @@ extern "C" int dg4_qkv_proj_lora(const dg4_layer_cfg* cfg, const void* packed, i
     int64_t down_at, up_at, gain_at;
     const int64_t need = dg4_lora_bytes(cfg->dtype, cfg->hidden, n_adapters, rank, &down_at, &up_at, &gain_at);
     if (!packed || ((uintptr_t)packed & 255) || packed_bytes < need) return DG4_EWORKSPACE;
-    if (row_end == row_begin) return DG4_OK;
+    const int64_t rows = row_end - row_begin;
+    if (rows == 0) return DG4_OK;
+    for (const void* out : { Q, K, V }) if (overlap(cfg, S, out, rows)) return DG4_EINVAL;
+    if (overlap(cfg, Q, K, rows) || overlap(cfg, Q, V, rows) || overlap(cfg, K, V, rows)) return DG4_EINVAL;
     dg4_lora_args a{};
     a.s = S; a.adapter = adapter;
     a.n_adapters = n_adapters; a.rank = rank;
@@ -410,6 +420,7 @@ extern "C" int dg4_kv8_read(const dg4_layer_cfg* cfg, int32_t format, const uint
     if (rc != DG4_OK) return rc;
     if (!K || !V || !aligned16(K, V)) return DG4_EINVAL;
     if (row_end == row_begin || n_store == 0) return DG4_OK;
+    if (overlap(cfg, K, V, row_end - row_begin)) return DG4_EINVAL;
     dg4_kv8_args a{};
     a.k_out = K; a.v_out = V;
     a.codes = const_cast<uint8_t*>(codes); a.scales = const_cast<uint8_t*>(scales); a.n_store = n_store;
@@ -428,6 +439,7 @@ extern "C" int dg4_sparse_attn_kv8_fwd(const dg4_layer_cfg* cfg, int32_t format,
     if (rc != DG4_OK) return rc;
     if (!Q || !rel_bias || !A || !aligned16(Q, A) || ((uintptr_t)rel_bias & 3) || g->hops != cfg->hops) return DG4_EINVAL;
     if (row_end == row_begin || g->n == 0) return DG4_OK;
+    if (A != Q && overlap(cfg, A, Q, row_end - row_begin)) return DG4_EINVAL;
     rc = dg4_graph_ensure_device(g);
     if (rc != DG4_OK) return rc;
     int dev = -1;

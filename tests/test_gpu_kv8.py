@@ -356,6 +356,19 @@ def test_captured_and_on_other_streams(hidden, dtype):
         assert all(torch.equal(a, b) for a, b in zip(got, out + [codes, scales])), step
 
 
+@pytest.mark.parametrize("hidden,dtype", [(128, "f32"), (256, "bf16")])
+@pytest.mark.parametrize("hops", [2, 3, 6])
+def test_attention_in_place(hidden, dtype, hops):
+    n = 3000 if hops < 6 else 500
+    g = circuit(n, 60, hops)
+    codes, scales = store(5, n, hidden, "e4m3")
+    Q = rows_of(6, n, hidden, dtype)
+    A, bias = torch.zeros_like(Q), torch.zeros((hidden // 32, 4), device="cuda")
+    dg4.dg4_sparse_attn_kv8_fwd(cfg(hidden, dtype, hops), "e4m3", g, Q, codes, scales, bias, A)
+    dg4.dg4_sparse_attn_kv8_fwd(cfg(hidden, dtype, hops), "e4m3", g, Q, codes, scales, bias, Q)
+    assert torch.equal(Q, A)
+
+
 def test_more_rows_than_a_launch_holds():
     c, n, rows = cfg(128, "bf16", 5), 400, 2 ** 26 + 5
     print(f"kv8 attention over {rows} rows, nearly all padding", flush=True)

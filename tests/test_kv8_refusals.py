@@ -28,6 +28,8 @@ def test_store_calls(call):
         assert call(**bad) == EINVAL, bad
     assert call(cfg=dg4.LayerConfig(64, 2, 2, 1, "f32")) == EUNSUPPORTED
     assert call(cfg=dg4.LayerConfig(128, 8, 2, 1, "f32")) == EUNSUPPORTED
+    if call is read:                               # rows of 512 bytes, four of them
+        assert call() == EINVAL and call(V=P + 2032) == EINVAL and call(K=P + 16) == EINVAL
     # nothing to do: fine, and nothing is looked at
     assert call(lo=2, hi=2) == 0
     assert call(lo=8, hi=8) == 0
@@ -47,6 +49,7 @@ def test_attention():
                 dict(hi=6), dict(lo=3, hi=1), dict(cfg=dg4.LayerConfig(128, 4, 3, 1, "bf16"))):
         assert call(**bad) == EINVAL, bad
     assert call(cfg=dg4.LayerConfig(96, 3, 2, 1, "bf16")) == EUNSUPPORTED
+    assert call(A=P + 256) == EINVAL and call(Q=P + 1264) == EINVAL           # (in place, or apart)
     assert call(lo=5, hi=5) == 0
 
 

@@ -52,6 +52,9 @@ def test_proj():
     for bad in (dict(packed=None), dict(packed=P + 128), dict(size=need - 1)):
         assert proj(**bad) == EWORKSPACE, bad
     assert proj() == 0 and proj(adapter=None) == 0 and proj(lo=7, hi=7) == 0
+    apart = dict(S=P, Q=2 * P, K=3 * P, V=4 * P)   # rows of 512 bytes
+    for bad in (dict(Q=P), dict(K=P + 4080), dict(V=2 * P + 16), dict(K=4 * P - 4080), dict(S=4 * P), dict(Q=3 * P + 512)):
+        assert proj(**{**apart, **bad}, hi=8) == EINVAL and proj(**{**apart, **bad}, lo=6, hi=14) == EINVAL, bad
     # no adapters: the rank is not looked at
     assert proj(n=0, rank=0, adapter=None) == 0 and proj(n=0, rank=900) == 0
 
