@@ -39,9 +39,9 @@ __device__ __forceinline__ int column_of(int m) { return 16 * ((m >> 2) & 1) + 4
 
 // Calls with up to so many elements of S split the columns over workgroups. Measured, split | not split, in us, rank 16:
 // bfloat16 at hidden 256, 4000 rows 8.8 | 9.9, 8000 rows 12.7 | 13.5, 10,000 rows 15.8 | 14.0; at 128, 4000 rows 5.5 | 9.7,
-// 14,000 rows 8.9 | 9.8; fp32 at 256, 4000 rows 28.9 | 43.9, 12,000 rows 61.8 | 65.0, 20,000 rows 96.5 | 93.9; at 128, 4000 rows
-// 11.7 | 15.0, 20,000 rows 29.6 | 31.4, 40,000 rows 52.0 | 49.7.
-template <typename T> constexpr int64_t SPREAD_ELEMENTS = sizeof(T) == 2 ? 1 << 21 : 1 << 22;
+// 14,000 rows 8.9 | 9.8; fp32 at 256, 4000 rows 28.9 | 43.9, 8000 rows 44.6 | 41.3, 16,000 rows 78.6 | 64.9; at 128, 4000 rows
+// 11.7 | 15.0, 12,000 rows 21.5 | 22.4, 16,000 rows 24.7 | 22.9, 24,000 rows 34.3 | 30.7.
+template <typename T> constexpr int64_t SPREAD_ELEMENTS = sizeof(T) == 2 ? 1 << 21 : 7 << 18;
 template <typename T> constexpr int PIECE = 16 / (int)sizeof(T);      // elements of 16 bytes
 inline int rank8(int rank) { return (rank + 7) / 8 * 8; }
 
@@ -180,79 +180,69 @@ struct Adapters {
     }
 };
 
-// T U_a for JT column tiles from `tile` on, on top of S W in the accumulators, two chunks of ranks at a time. A tile of rows with
-// one adapter has its first two chunks requested ahead, by first(). Otherwise adapter after adapter, a column tile at a time, the
-// next two chunks (of the same adapter or the next) requested before these are multiplied; the sums are kept for its own rows.
-template <typename T, int D, int JT> struct UpProduct {
-    uint4 up[2][JT];
-    template <int N>
-    __device__ __forceinline__ static void fetch(const dg4_lora_args& p, int a, int c0, int tile, int n, int hi, uint4 (&to)[2][N])
+// Chunk c of T as operand: bfloat16 has the high parts of eight ranks in one half of the wave and their low parts in the other,
+// against the same eight rows of U_a
+template <typename T> __device__ __forceinline__ uint4 low_operand(const dg4_lora_args& p, const T* low, int c, int n, int hi)
+{
+    const T* row = low + n * low_stride<T>(p.rank8);
+    return *(const uint4*)(sizeof(T) == 2 ? row + hi * p.rank8 + c * 8 : row + (2 * c + hi) * 4);
+}
+
+// T U_a for a column tile, on top of S W in the accumulators, two chunks of ranks at a time. A tile of rows with one adapter has its
+// first two chunks requested ahead, by first(). Otherwise adapter after adapter, the next two chunks (of the same adapter or the
+// next) requested before these are multiplied; the sums are kept for its own rows.
+template <typename T, int D> struct UpProduct {
+    uint4 up[2];
+    __device__ __forceinline__ static void fetch(const dg4_lora_args& p, int a, int c0, int tile, int n, int hi, uint4 (&to)[2])
     {
         constexpr int E = PIECE<T>;
         const int chunks = p.rank8 / RANKS;
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             const int at = min(c0 + c, chunks - 1), unit = sizeof(T) == 2 ? at : 2 * at + hi;
-            const uint4* src = (const uint4*)p.up_packed + ((int64_t)a * (p.rank8 / E) + unit) * (3 * D) + tile * 32 + column_of(n);
-#pragma unroll
-            for (int j = 0; j < N; ++j) to[c][j] = src[j * 32];
+            to[c] = ((const uint4*)p.up_packed)[((int64_t)a * (p.rank8 / E) + unit) * (3 * D) + tile * 32 + column_of(n)];
         }
     }
     __device__ __forceinline__ void first(const dg4_lora_args& p, const Adapters& ad, int tile, int n, int hi)
     {
         if (ad.any && ad.one) fetch(p, ad.first, 0, tile, n, hi, up);
     }
-    // chunk c of T as operand: bfloat16 has the high parts of eight ranks in one half of the wave and their low parts in the
-    // other, against the same eight rows of U_a
-    __device__ __forceinline__ static uint4 low_operand(const dg4_lora_args& p, const T* low, int c, int n, int hi)
-    {
-        const T* row = low + n * low_stride<T>(p.rank8);
-        return *(const uint4*)(sizeof(T) == 2 ? row + hi * p.rank8 + c * 8 : row + (2 * c + hi) * 4);
-    }
-    __device__ __forceinline__ void run_one(const dg4_lora_args& p, const Adapters& ad, const T* low, int tile, int n, int hi, f32x16 (&acc)[JT])
+    __device__ __forceinline__ void run_one(const dg4_lora_args& p, const Adapters& ad, const T* low, int tile, int n, int hi, f32x16& acc)
     {
         const int chunks = p.rank8 / RANKS;
         for (int c0 = 0; c0 < chunks; c0 += 2) {
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                if (c0 + c < chunks) {
-                    const uint4 b = low_operand(p, low, c0 + c, n, hi);
-#pragma unroll
-                    for (int j = 0; j < JT; ++j) Mma<T>::run(up[c][j], b, acc[j]);
-                }
-            }
+            for (int c = 0; c < 2; ++c)
+                if (c0 + c < chunks) Mma<T>::run(up[c], low_operand(p, low, c0 + c, n, hi), acc);
             if (c0 + 2 < chunks) fetch(p, ad.first, c0 + 2, tile, n, hi, up);
         }
     }
-    __device__ __forceinline__ static void run_mixed(const dg4_lora_args& p, const Adapters& ad, const T* low, int tile, int n, int hi, f32x16 (&acc)[JT])
+    __device__ __forceinline__ static void run_mixed(const dg4_lora_args& p, const Adapters& ad, const T* low, int tile, int n, int hi, f32x16& acc)
     {
         const int chunks = p.rank8 / RANKS;
+        uint64_t todo = __ballot(ad.mine >= 0);
+        int a = __builtin_amdgcn_readlane(ad.mine, (int)__builtin_ctzll(todo));
+        todo &= ~__ballot(ad.mine == a);
+        uint4 now[2], next[2];
+        fetch(p, a, 0, tile, n, hi, now);
+        f32x16 part = acc;                        // (S W for the rows whose turn has not come; the others are not kept again)
+        for (int c0 = 0;;) {
+            const bool ends = c0 + 2 >= chunks, more = !ends || todo != 0;
+            const int a_next = ends && todo ? __builtin_amdgcn_readlane(ad.mine, (int)__builtin_ctzll(todo)) : a;
+            if (more) fetch(p, a_next, ends ? 0 : c0 + 2, tile, n, hi, next);
 #pragma unroll
-        for (int j = 0; j < JT; ++j) {
-            uint64_t todo = __ballot(ad.mine >= 0);
-            int a = __builtin_amdgcn_readlane(ad.mine, (int)__builtin_ctzll(todo));
-            todo &= ~__ballot(ad.mine == a);
-            uint4 now[2][1], next[2][1];
-            fetch(p, a, 0, tile + j, n, hi, now);
-            f32x16 part = acc[j];                 // (S W for the rows whose turn has not come; the others are not kept again)
-            for (int c0 = 0;;) {
-                const bool ends = c0 + 2 >= chunks, more = !ends || todo != 0;
-                const int a_next = ends && todo ? __builtin_amdgcn_readlane(ad.mine, (int)__builtin_ctzll(todo)) : a;
-                if (more) fetch(p, a_next, ends ? 0 : c0 + 2, tile + j, n, hi, next);
+            for (int c = 0; c < 2; ++c)
+                if (c0 + c < chunks) Mma<T>::run(now[c], low_operand(p, low, c0 + c, n, hi), part);
+            if (ends) {
 #pragma unroll
-                for (int c = 0; c < 2; ++c)
-                    if (c0 + c < chunks) Mma<T>::run(now[c][0], low_operand(p, low, c0 + c, n, hi), part);
-                if (ends) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) acc[j][i] = ad.mine == a ? part[i] : acc[j][i];
-                    part = acc[j];
-                }
-                if (!more) break;
-                now[0][0] = next[0][0]; now[1][0] = next[1][0];
-                c0 = ends ? 0 : c0 + 2;
-                todo &= ~__ballot(ad.mine == a_next);
-                a = a_next;
+                for (int i = 0; i < 16; ++i) acc[i] = ad.mine == a ? part[i] : acc[i];
+                part = acc;
             }
+            if (!more) break;
+            now[0] = next[0]; now[1] = next[1];
+            c0 = ends ? 0 : c0 + 2;
+            todo &= ~__ballot(ad.mine == a_next);
+            a = a_next;
         }
     }
 };
@@ -306,29 +296,28 @@ __device__ __forceinline__ void put_tiles(const Outputs& to, const f32x16* acc, 
 }
 
 // LDS of the streaming kernel, in bytes: the rows, T, rows on their way out
-template <typename T, int D, int TILES_OUT> struct StreamLds {
+template <typename T, int D> struct StreamLds {
     static constexpr int S_STRIDE = D + PIECE<T>;                                  // elements
     static constexpr int S_BYTES = ROWS * S_STRIDE * (int)sizeof(T);
-    static constexpr int O_STRIDE = TILES_OUT * 32 + PIECE<T>;
+    static constexpr int O_STRIDE = 32 + PIECE<T>;
     __host__ __device__ static constexpr int out_at(int r8) { return S_BYTES + ROWS * low_stride<T>(r8) * (int)sizeof(T); }
     __host__ __device__ static constexpr int bytes(int r8) { return out_at(r8) + 4 * ROWS * O_STRIDE * (int)sizeof(T); }
 };
 
-// A workgroup of four waves takes a tile of rows, a wave JT column tiles at a time: weights arrive from the L2 a few chunks before
-// they are multiplied, the next pass's among them, and two workgroups to a compute unit fill each other's waits. SPREAD, for
+// A workgroup of four waves takes a tile of rows, a wave one column tile after the other: weights arrive from the L2 a few chunks before
+// they are multiplied, the next pass's among them, and two or three workgroups to a compute unit fill each other's waits. SPREAD, for
 // calls with few rows, where latency counts: a wave takes one column tile, the others go to 3D/32/4 workgroups along y, and a
 // tile holds p.tile_rows <= 32 rows (the rest of its operand repeats the last).
 // Measured, rank 16: 64 rows of bfloat16 at hidden 256, each with its own adapter, 5.2 us, waits of memory after one another
 // (adapters, D_a, U_a) and two products that hang on each other; 20,257 rows of fp32 at 128 in 28 us, 77 TFLOP/s, bound by the
-// matrix cores, half of the library's 153 on a large product (a tile's start and end have nothing to multiply, and T is formed in
-// each of the three workgroups); 150,000 rows of fp32 at 256 in 548 us, 120 TFLOP/s.
-template <typename T, int D, int JT, bool SPREAD>
+// matrix cores of the compute units that get three tiles (634 tiles on 256; a tile is some 7 us of products); 150,000 rows of fp32
+// at 256 in 548 us, 120 TFLOP/s. Two or three column tiles to a wave at once are no faster (552; at 128, 24,000 rows 34 for 31),
+// nor are three workgroups to a compute unit with D_a fetched where it is used (555).
+template <typename T, int D, bool SPREAD>
 __global__ __launch_bounds__(256, 2) void lora_stream_kernel(dg4_lora_args p)
 {
-    constexpr int E = PIECE<T>, KC = D / (2 * E), TILES = 3 * D / 32, PASSES = SPREAD ? 1 : TILES / 4 / JT;
-    static_assert(SPREAD ? JT == 1 : TILES % (4 * JT) == 0, "column tiles");
-    constexpr int TILES_OUT = sizeof(T) == 2 ? JT : 1;         // column tiles that leave together (128 bytes of a row)
-    using L = StreamLds<T, D, TILES_OUT>;
+    constexpr int E = PIECE<T>, KC = D / (2 * E), TILES = 3 * D / 32, PASSES = SPREAD ? 1 : TILES / 4;
+    using L = StreamLds<T, D>;
     constexpr int RING = sizeof(T) == 2 ? 8 : 4;  // chunks of weights requested ahead
     static_assert(KC % RING == 0, "the ring's place of a chunk is the same in every pass");
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
@@ -353,13 +342,11 @@ __global__ __launch_bounds__(256, 2) void lora_stream_kernel(dg4_lora_args p)
         const int piece = (int)threadIdx.x + 256 * i;
         row_piece[i] = *((const uint4*)((const T*)p.s + row_at(piece / CPR) * D) + piece % CPR);
     }
-    const int tile0 = SPREAD ? (int)blockIdx.y * 4 + wave : wave * PASSES * JT;
+    const int tile0 = SPREAD ? (int)blockIdx.y * 4 + wave : wave * PASSES;
     const uint4* wp = (const uint4*)p.w_packed + (int64_t)tile0 * KC * 64 + lane;
-    uint4 ring[RING][JT];
+    uint4 ring[RING];
 #pragma unroll
-    for (int c = 0; c < RING; ++c)
-#pragma unroll
-        for (int j = 0; j < JT; ++j) ring[c][j] = wp[(j * KC + c) * 64];
+    for (int c = 0; c < RING; ++c) ring[c] = wp[c * 64];
 
     Adapters ad;
     ad.set(id, p.n_adapters);
@@ -370,7 +357,7 @@ __global__ __launch_bounds__(256, 2) void lora_stream_kernel(dg4_lora_args p)
     const bool down_ahead = ad16.any && ad16.one && wave / 2 * 16 < p.rank;
     uint4 d[DOWN_STEPS<T, D>];
     if (down_ahead) fetch_down<T, D>(p, ad16.first, wave / 2 * 16, lane, d);
-    UpProduct<T, D, JT> up;
+    UpProduct<T, D> up;
     up.first(p, ad, tile0, n, hi);
     const float gain = ad16.mine >= 0 ? p.gain_packed[ad16.mine] : 0.f;
 #pragma unroll
@@ -384,24 +371,18 @@ __global__ __launch_bounds__(256, 2) void lora_stream_kernel(dg4_lora_args p)
     // (unrolled, so that the weights on their way are waited for one by one and not behind the stores of a pass)
 #pragma unroll
     for (int pass = 0; pass < PASSES; ++pass) {
-        f32x16 acc[JT];
+        f32x16 acc;
 #pragma unroll
-        for (int j = 0; j < JT; ++j)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[j][i] = 0.f;
-        const int tile = tile0 + pass * JT;
+        for (int i = 0; i < 16; ++i) acc[i] = 0.f;
+        const int tile = tile0 + pass;
         uint4 b[2];                               // rows as operand: this chunk's and the next's
         b[0] = row_operand(0);
 #pragma unroll
         for (int c = 0; c < KC; ++c) {
             if (c + 1 < KC) b[(c + 1) & 1] = row_operand(c + 1);
-#pragma unroll
-            for (int j = 0; j < JT; ++j) Mma<T>::run(ring[c % RING][j], b[c & 1], acc[j]);
+            Mma<T>::run(ring[c % RING], b[c & 1], acc);
             const int ahead = pass * KC + c + RING;            // chunk, on through the passes
-            if (ahead < PASSES * KC) {
-#pragma unroll
-                for (int j = 0; j < JT; ++j) ring[c % RING][j] = wp[((ahead / KC * JT + j) * KC + ahead % KC) * 64];
-            }
+            if (ahead < PASSES * KC) ring[c % RING] = wp[ahead * 64];
             __builtin_amdgcn_sched_barrier(0);
         }
         if (ad.any) {
@@ -423,9 +404,8 @@ __global__ __launch_bounds__(256, 2) void lora_stream_kernel(dg4_lora_args p)
             if (ad.one) up.run_one(p, ad, low, tile, n, hi, acc);
             else up.run_mixed(p, ad, low, tile, n, hi, acc);
         }
-        if (pass + 1 < PASSES) up.first(p, ad, tile + JT, n, hi);
-#pragma unroll
-        for (int j = 0; j < JT; j += TILES_OUT) put_tiles<T, D, TILES_OUT, L::O_STRIDE>(outputs, acc + j, out_rows, r0, r_end, tile + j, lane);
+        if (pass + 1 < PASSES) up.first(p, ad, tile + 1, n, hi);
+        put_tiles<T, D, 1, L::O_STRIDE>(outputs, &acc, out_rows, r0, r_end, tile, lane);
     }
 }
 
@@ -615,7 +595,7 @@ __global__ __launch_bounds__(512, 2) void lora_resident_kernel(dg4_lora_args p)
                 for (int c = 0; c < 2; ++c) {
                     const int at = min(c0 + c, chunks - 1);
 #pragma unroll
-                    for (int t = 0; t < COUNT; ++t) x[c][t] = UpProduct<T, D, JT>::low_operand(p, low + (t0 + t) * ROWS * low_stride<T>(p.rank8), at, n, hi);
+                    for (int t = 0; t < COUNT; ++t) x[c][t] = low_operand(p, low + (t0 + t) * ROWS * low_stride<T>(p.rank8), at, n, hi);
 #pragma unroll
                     for (int j = 0; j < JT; ++j) y[c][j] = up_held[(at * JT + j) * 32 + n];
                 }
@@ -691,11 +671,11 @@ int launch_proj(dg4_lora_args a, hipStream_t s)
 {
     const int64_t rows = a.row_end - a.row_begin;
     if (rows * D <= SPREAD_ELEMENTS<T>) {
-        const auto kernel = lora_stream_kernel<T, D, 1, true>;
+        const auto kernel = lora_stream_kernel<T, D, true>;
         // rows per tile: few enough for two workgroups per compute unit
         a.tile_rows = 1;
         while (a.tile_rows < ROWS && rows * (3 * D / 128) > (int64_t)512 * a.tile_rows) a.tile_rows *= 2;
-        const int smem = StreamLds<T, D, 1>::bytes(a.rank8);
+        const int smem = StreamLds<T, D>::bytes(a.rank8);
         if (const int e = allow_lds(kernel, smem); e != hipSuccess) return e;
         hipLaunchKernelGGL(kernel, dim3((unsigned)((rows + a.tile_rows - 1) / a.tile_rows), 3 * D / 128), dim3(256), smem, s, a);
     } else if constexpr (sizeof(T) == 2) {
@@ -710,9 +690,8 @@ int launch_proj(dg4_lora_args a, hipStream_t s)
         const int64_t walks = std::min<int64_t>(std::max(1, cus / PARTS), (rows + L::TILE - 1) / L::TILE);
         hipLaunchKernelGGL(kernel, dim3((unsigned)(PARTS * walks)), dim3(512), smem, s, a);
     } else {
-        constexpr int JT = D == 256 ? 2 : 3;
-        const auto kernel = lora_stream_kernel<T, D, JT, false>;
-        const int smem = StreamLds<T, D, 1>::bytes(a.rank8);
+        const auto kernel = lora_stream_kernel<T, D, false>;
+        const int smem = StreamLds<T, D>::bytes(a.rank8);
         if (const int e = allow_lds(kernel, smem); e != hipSuccess) return e;
         hipLaunchKernelGGL(kernel, dim3((unsigned)((rows + ROWS - 1) / ROWS)), dim3(256), smem, s, a);
     }
