@@ -373,6 +373,11 @@ def _call(where: str, cfg: LayerConfig, first):
     return _types[cfg.dtype], dev, _raw_stream(dev)
 
 
+def _shape(cfg: LayerConfig):
+    """What the serving calls look at of a configuration, for the C call (its flags are dg4_layer_fwd's)."""
+    return ctypes.byref(_Cfg(cfg.hidden, cfg.heads, cfg.hops, 1, DG4_F32 if cfg.dtype == "f32" else DG4_BF16))
+
+
 @dataclass
 class LoraWeights:
     """Shared projection and adapters in matrix-core operand order (dg4_lora_pack); read only from then on."""
@@ -384,8 +389,7 @@ class LoraWeights:
 
 
 def dg4_lora_packed_bytes(cfg: LayerConfig, n_adapters: int, rank: int) -> int:
-    c = cfg.c()
-    r = lib().dg4_lora_packed_bytes(ctypes.byref(c), n_adapters, rank)
+    r = lib().dg4_lora_packed_bytes(_shape(cfg), n_adapters, rank)
     if r < 0:
         raise DG4Error(int(r), "dg4_lora_packed_bytes")
     return int(r)
@@ -404,8 +408,7 @@ def dg4_lora_pack(cfg: LayerConfig, Wqkv, Down=None, Up=None, gain=None) -> Lora
             _refused(Up, td, dev, 3 * n * d * rank) or gain is not None and _refused(gain, _types["f32"], dev, n)):
         raise DG4Error(-1, where)
     packed = _ws(dg4_lora_packed_bytes(cfg, n, rank), Wqkv)
-    c = cfg.c()
-    rc = lib().dg4_lora_pack(ctypes.byref(c), Wqkv.data_ptr(), n, rank, Down.data_ptr() if n else None,
+    rc = lib().dg4_lora_pack(_shape(cfg), Wqkv.data_ptr(), n, rank, Down.data_ptr() if n else None,
                              Up.data_ptr() if n else None, gain.data_ptr() if n and gain is not None else None,
                              packed.data_ptr(), packed.numel(), stream)
     _check(rc, where)
@@ -425,8 +428,7 @@ def dg4_qkv_proj_lora(cfg: LayerConfig, weights: LoraWeights, S, adapter, Q, K, 
     if row_begin == row_end == 0:                # (an empty tensor has no address)
         return
     packed = weights.packed
-    c = cfg.c()
-    rc = lib().dg4_qkv_proj_lora(ctypes.byref(c), packed.data_ptr(), packed.numel(), weights.n_adapters, weights.rank,
+    rc = lib().dg4_qkv_proj_lora(_shape(cfg), packed.data_ptr(), packed.numel(), weights.n_adapters, weights.rank,
                                  S.data_ptr(), row_begin, row_end, adapter.data_ptr() if adapter is not None else None,
                                  Q.data_ptr(), K.data_ptr(), V.data_ptr(), stream)
     _check(rc, where)
@@ -438,9 +440,12 @@ def _store_call(where: str, cfg: LayerConfig, fmt: str, codes, scales, ids, x, y
     td, dev, stream = _call(where, cfg, codes)
     n, rows = codes.shape[0], x.shape[0]
     row_end = rows if row_end is None else row_end
-    if (fmt not in KV_FORMATS or row_end > rows or _refused(x, td, dev, rows * cfg.hidden) or
-            _refused(y, td, dev, rows * cfg.hidden) or _refused(codes, _types["bytes"], dev, n * 2 * cfg.hidden) or
-            _refused(scales, _types["bytes"], dev, n * 2 * cfg.heads) or scales.shape != (n, cfg.heads, 2) or
+    k, byte = rows * cfg.hidden, _types["bytes"]               # (_refused of each, without the calls: a level's call is short)
+    if (fmt not in KV_FORMATS or row_end > rows or x.dtype is not td or y.dtype is not td or codes.dtype is not byte or
+            scales.dtype is not byte or x.numel() != k or y.numel() != k or codes.numel() != n * 2 * cfg.hidden or
+            scales.shape != (n, cfg.heads, 2) or not (x.is_contiguous() and y.is_contiguous() and codes.is_contiguous() and
+                                                      scales.is_contiguous()) or
+            x.get_device() != dev or y.get_device() != dev or scales.get_device() != dev or
             ids is not None and _refused(ids, _types["ids"], dev, rows)):
         raise DG4Error(-1, where)
     if row_begin == row_end == 0 or n == 0 and ids is not None:      # (an empty tensor has no address)
@@ -454,8 +459,7 @@ def dg4_kv8_write(cfg: LayerConfig, fmt: str, K, V, codes, scales, ids=None, row
     f, row_end, n, ip, stream = _store_call("dg4_kv8_write", cfg, fmt, codes, scales, ids, K, V, row_begin, row_end)
     if f is None:
         return
-    c = cfg.c()
-    rc = lib().dg4_kv8_write(ctypes.byref(c), f, K.data_ptr(), V.data_ptr(), row_begin, row_end, ip, codes.data_ptr(),
+    rc = lib().dg4_kv8_write(_shape(cfg), f, K.data_ptr(), V.data_ptr(), row_begin, row_end, ip, codes.data_ptr(),
                              scales.data_ptr(), n, stream)
     _check(rc, "dg4_kv8_write")
 
@@ -465,8 +469,7 @@ def dg4_kv8_read(cfg: LayerConfig, fmt: str, codes, scales, K, V, ids=None, row_
     f, row_end, n, ip, stream = _store_call("dg4_kv8_read", cfg, fmt, codes, scales, ids, K, V, row_begin, row_end)
     if f is None:
         return
-    c = cfg.c()
-    rc = lib().dg4_kv8_read(ctypes.byref(c), f, codes.data_ptr(), scales.data_ptr(), n, ip, row_begin, row_end,
+    rc = lib().dg4_kv8_read(_shape(cfg), f, codes.data_ptr(), scales.data_ptr(), n, ip, row_begin, row_end,
                             K.data_ptr(), V.data_ptr(), stream)
     _check(rc, "dg4_kv8_read")
 
@@ -479,8 +482,7 @@ def dg4_sparse_attn_kv8_fwd(cfg: LayerConfig, fmt: str, g: Graph, Q, codes, scal
         raise DG4Error(-1, "dg4_sparse_attn_kv8_fwd")
     if f is None:
         return
-    c = cfg.c()
-    rc = lib().dg4_sparse_attn_kv8_fwd(ctypes.byref(c), f, g.handle, row_begin, row_end, ip, Q.data_ptr(), codes.data_ptr(),
+    rc = lib().dg4_sparse_attn_kv8_fwd(_shape(cfg), f, g.handle, row_begin, row_end, ip, Q.data_ptr(), codes.data_ptr(),
                                        scales.data_ptr(), rel_bias.data_ptr(), A.data_ptr(), stream)
     _check(rc, "dg4_sparse_attn_kv8_fwd")
 
