@@ -273,9 +273,10 @@ template <> struct LaneQ<bf16_t, DG4_KV_E4M3> {
 // addressing are 32 bits: FAR, for larger stores, has addresses of 64 bits and reads zeros from memory for them.
 // Up to eight entries a row are two groups of four (2,4: one group of eight 504 us for a million two-hop rows of bfloat16 at 256,
 // two of four 491 us, before the rows were grouped by XCD), up to sixteen two of eight; longer rows have a whole wave, whose groups
-// keep their loads in flight (15,135 rows of eight-hop cones of bfloat16 at 128: 62 us).
+// keep their loads in flight (15,135 rows of eight-hop cones of bfloat16 at 128: 58.6 us, 61.6 where each step moves on to its maximum).
 // Measured: 450 us for that million rows, 2.34 GB fetched and 0.51 written (6.3 TB/s) where the store, Q, the table and A are 1.6 GB:
-// bound by sources that several XCDs fetch. Long rows are bound by conversions, 4 cycles for two codes of e4m3 and 8 of int8. 20,256 rows of fp32 at 128,
+// bound by sources that several XCDs fetch. Long rows are bound by vector instructions (busy 89 % of the cycles), 64
+// for an entry in bfloat16 / e4m3: 16 conversions, 8 and 16 products, and what finds, scales and weighs it. 20,256 rows of fp32 at 128,
 // int8: 8.3 us. One row: 2.5 us, three waits of memory after one another.
 template <typename T, int FMT, int D, int S, int CH, bool ONCE, bool FAR>
 __global__ __launch_bounds__(256) void kv8_attn_kernel(dg4_kv8_attn_args p)
@@ -309,7 +310,7 @@ __global__ __launch_bounds__(256) void kv8_attn_kernel(dg4_kv8_attn_args p)
     LaneQ<T, FMT> q;
     q.load((const T*)p.q + r * D + sub * 16);
     const float c = 0.17677669529663687f;         // 1/sqrt(32)
-    const float log2e = 1.4426950408889634f;
+    const float log2e = 1.4426950408889634f;      // (not taken into the scores: the lowest bias times this is no number)
     float m = -INFINITY, z = 0.f;
     float acc[16];
     if constexpr (!ONCE) {
@@ -351,17 +352,23 @@ __global__ __launch_bounds__(256) void kv8_attn_kernel(dg4_kv8_attn_args p)
             s[j] = fmaf(dot, FMT == DG4_KV_E4M3 ? c : scale_value(sw[j] & 255u) * c, b[j]);
             cm = fmaxf(cm, s[j]);
         }
-        // (nothing so far: any finite base will do, every weight is 0)
-        const float base = cm == -INFINITY ? 0.f : cm;
-        if constexpr (!ONCE) {
-            const float corr = __builtin_amdgcn_exp2f((m - base) * log2e);
+        // What weights are relative to: the maximum; in a wave with steps to come (one row) what it was when some lane's last was more
+        // than 4 past it, so that few steps have sums to scale down. e^4 < 2^6, which every weight there is divided by: no sum of V is
+        // larger than it would be, and a source alone in its row still leaves as it is.
+        // (Nothing so far, -inf: any finite base will do, every weight is 0.)
+        if constexpr (ONCE) {
+            m = cm;
+        } else if (__any(cm > m + 4.f)) {
+            const float corr = __builtin_amdgcn_exp2f((m - (cm == -INFINITY ? 0.f : cm)) * log2e);
+            m = cm;
             z *= corr;
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[i] *= corr;
         }
+        const float base = m == -INFINITY ? 0.f : m;
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
-            const float pj = __builtin_amdgcn_exp2f((s[j] - base) * log2e);
+            const float pj = __builtin_amdgcn_exp2f(ONCE ? (s[j] - base) * log2e : fmaf(s[j] - base, log2e, -6.f));
             z += pj;
             const float pv = FMT == DG4_KV_E4M3 ? pj : pj * scale_value(sw[j] >> 8);
             const uint32_t words[4] = { vw[j].x, vw[j].y, vw[j].z, vw[j].w };
@@ -373,7 +380,6 @@ __global__ __launch_bounds__(256) void kv8_attn_kernel(dg4_kv8_attn_args p)
                 for (int k = 0; k < 4; ++k) acc[4 * i + k] = ONCE && j == 0 ? pv * x[k] : fmaf(pv, x[k], acc[4 * i + k]);
             }
         }
-        m = cm;
         if constexpr (ONCE) break;
     }
     // join the groups of the row: one maximum, then sums, each exchange leaving a lane half the features it had

@@ -356,6 +356,33 @@ def test_captured_and_on_other_streams(hidden, dtype):
         assert all(torch.equal(a, b) for a, b in zip(got, out + [codes, scales])), step
 
 
+@pytest.mark.parametrize("hidden,dtype", [(128, "f32"), (256, "bf16"), (256, "f32"), (128, "bf16")])
+@pytest.mark.parametrize("span", [-300.0, -40.0, 9.0, 40.0, 300.0])
+def test_scores_that_rise_or_fall_along_a_row(hidden, dtype, span):
+    """Long rows in ascending id: the maximum moves on in every step, in a few, or stays with the first; V up to 2^118."""
+    n, hops = 1200, 8
+    g = circuit(n, 200, hops)
+    assert np.diff(g.array("nbr_ptr")).max() > 96               # (more than three steps)
+    codes, scales = store(12, n, hidden, "int8")
+    rise = torch.linspace(0, 1, n, device="cuda")[:, None] * (span / 32 * np.sqrt(32)) + torch.zeros((n, hidden), device="cuda")
+    V = rows_of(13, n, hidden, "f32")
+    dg4.dg4_kv8_write(cfg(hidden, "f32"), "int8", rise, V, codes, scales)
+    Q = torch.ones((n, hidden), device="cuda").to(tdtype(dtype))
+    bias = torch.zeros((hidden // 32, 4), device="cuda")
+    want, bound = reference(g, range(n), Q, codes, scales, "int8", bias, dtype)
+    # Powers below 2^-126, the smallest normal number, may count as zero, those of weights (relative to a base that is at most 4
+    # below the maximum, e^4 < 2^6, and divided by 2^6) and those that join two bases: a source loses at most 2^-126 * 2^6 of the
+    # largest weight, and the sum of weights is at least that. Blocks of 2^110 show it: with weights below 2^-126 taken out, the
+    # 64-bit result itself is 1413 times the bound above away (row 1153, span -300).
+    V = ref.values(codes.cpu().numpy(), scales.cpu().numpy(), "int8")[1]
+    ptr, idx = g.array("nbr_ptr"), g.array("nbr_idx")
+    bound = bound + 2.0 ** -120 * np.stack([np.abs(V[idx[ptr[v]:ptr[v + 1]]]).sum(0) for v in range(n)])
+    A = torch.full_like(Q, 7.0)
+    dg4.dg4_sparse_attn_kv8_fwd(cfg(hidden, dtype, hops), "int8", g, Q, codes, scales, bias, A)
+    err = np.abs(to_np(A) - want)
+    assert (err <= bound).all(), (err / bound).max()
+
+
 @pytest.mark.parametrize("hidden,dtype", [(128, "f32"), (256, "bf16")])
 @pytest.mark.parametrize("hops", [2, 3, 6])
 def test_attention_in_place(hidden, dtype, hops):
