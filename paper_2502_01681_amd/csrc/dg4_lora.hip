@@ -135,13 +135,16 @@ template <typename T> __device__ __forceinline__ void put_low(T* row, int q, int
 #pragma unroll
     for (int k = 0; k < 4; ++k) v[k] = q + k < rank ? sum[k] * gain : 0.f;
     if constexpr (sizeof(T) == 2) {
+        // The high part is cut off towards zero, strictly below v, so that the low part is not zero and has v's sign: where a
+        // number of U_a is infinite, both products are the infinity that v times it is. What is left out is at most 2^-16 of v.
+        // (Rounded to nearest, the parts gave a NaN there wherever the low one was zero or had the other sign, and a high part of
+        // infinity from 3.396e38 on.) An infinity is the largest number and an infinity; a NaN stays one.
         uint32_t h[4];
         float rest[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            h[k] = f32_to_bf16_bits(v[k]);
-            const float back = __uint_as_float(h[k] << 16);
-            rest[k] = fabsf(back) < INFINITY ? v[k] - back : 0.f;                  // (an infinity has no low part)
+            h[k] = v[k] == 0.f ? 0u : (__float_as_uint(v[k]) - 1u) >> 16;
+            rest[k] = v[k] - __uint_as_float(h[k] << 16);
         }
         *(uint2*)(row + q) = make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
         *(uint2*)(row + r8 + q) = make_uint2(pack_bf16x2(rest[0], rest[1]), pack_bf16x2(rest[2], rest[3]));
