@@ -349,6 +349,8 @@ __global__ __launch_bounds__(256) void kv8_attn_kernel(dg4_kv8_attn_args p)
         for (int j = 0; j < CH; ++j) {
             float dot = q.dot(kw[j], sw[j] & 255u);
             dot += xor1(dot);
+            // (zeros times a q that is not finite are NaN: an entry that is none has no product)
+            dot = b[j] == -INFINITY ? 0.f : dot;
             s[j] = fmaf(dot, FMT == DG4_KV_E4M3 ? c : scale_value(sw[j] & 255u) * c, b[j]);
             cm = fmaxf(cm, s[j]);
         }

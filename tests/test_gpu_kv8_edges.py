@@ -1,0 +1,44 @@
+"""Attention over the 8-bit store where rows of Q or values of the store are at the end of their type's range."""
+import numpy as np
+import pytest
+import torch
+
+import kv8_ref as ref
+import paper_2502_01681_amd as dg4
+from gpu_utils import tdtype, to_np
+from test_gpu_kv8 import HALF_STEP, cfg, circuit, reference, store
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("hidden,dtype", [(128, "f32"), (256, "bf16"), (256, "f32"), (128, "bf16")])
+@pytest.mark.parametrize("hops", [1, 3, 5, 8])
+def test_a_head_without_sources_gives_zeros_whatever_q_holds(fmt, hidden, dtype, hops):
+    """Head 0 leaves everything out, head 1 the gate itself (all that a primary input has). Rows of Q in turn: finite, with a
+    NaN, an infinity, a negative infinity in every head."""
+    n = 120
+    print(f"kv8 Q that is not finite {fmt} {hidden} {dtype} hops={hops}", flush=True)
+    g = circuit(n, 60, hops, seed=2)
+    codes, scales = store(6, n, hidden, fmt)
+    rng = np.random.default_rng(7)
+    finite = torch.from_numpy(rng.standard_normal((n, hidden)).astype(np.float32)).to(tdtype(dtype)).cuda()
+    bias = torch.zeros((hidden // 32, 4), device="cuda")
+    bias[0] = -np.inf
+    bias[1, 0] = -np.inf
+    Q = finite.clone().view(n, -1, 32)
+    for kind, x in ((1, "nan"), (2, "inf"), (3, "-inf")):
+        Q[kind::4, :, 5 + kind] = float(x)
+    Q = Q.view(n, hidden)
+    A, B = torch.full_like(Q, 7.0), torch.full_like(Q, 7.0)
+    dg4.dg4_sparse_attn_kv8_fwd(cfg(hidden, dtype, hops), fmt, g, finite, codes, scales, bias, A)
+    dg4.dg4_sparse_attn_kv8_fwd(cfg(hidden, dtype, hops), fmt, g, Q, codes, scales, bias, B)
+    assert torch.equal(A[::4], B[::4])             # (a row does not see its neighbours)
+    single = torch.from_numpy(np.diff(g.array("nbr_ptr")) == 1).cuda()
+    assert int(single[1::4].sum()) and int(single[2::4].sum()) and int(single[3::4].sum())
+    assert (B[:, :32] == 0).all()
+    assert (B[single][:, 32:64] == 0).all()
+    # with a source left, a NaN in Q is a NaN in the head
+    assert B[1::4, 64:].isnan().all() and B[1::4][~single[1::4]][:, 32:64].isnan().all()
+    want, bound = reference(g, range(0, n, 4), finite[::4], codes, scales, fmt, bias, dtype)
+    assert (np.abs(to_np(B[::4]) - want) <= bound).all()
