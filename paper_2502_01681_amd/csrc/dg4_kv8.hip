@@ -220,9 +220,15 @@ template <int FMT> __device__ __forceinline__ void decode4_scaled(uint32_t w, ui
     }
 }
 
-// A lane's sixteen values of q, and their product with as many codes (without the scale in int8). bfloat16 against e4m3:
-// pairs of bfloat16 numbers, which hold a code times its power of two exactly, two products and a sum in fp32 per instruction.
+// A lane's sixteen values of q, and their product with as many codes. dot: in fp32 / e4m3 with the codes' power of two; in int8
+// without it, for the whole sum to be multiplied by; bfloat16 against e4m3 as pairs of bfloat16 numbers, a code times its power of
+// two, two products and a sum in fp32 per instruction. The two short forms have their ends: sums of q times codes overflow from
+// |q| = 2^116 on, and such an instruction takes what is below 2^-126, as a code times 2^-117 and less may be, as zero. Up to LARGE_Q
+// the one does not happen and the other costs a score at most 32 * 2^-126 * LARGE_Q = 2^-41; rows of Q that go further take
+// dot_large, every value of K in fp32 (which holds it exactly).
+constexpr uint32_t LARGE_Q = (127u + 80u) << 23;              // 2^80, as a float's bits
 template <typename T, int FMT> struct LaneQ {
+    static constexpr bool SHORT = FMT != DG4_KV_E4M3;
     float q[16];
     __device__ __forceinline__ void load(const T* p)
     {
@@ -233,6 +239,13 @@ template <typename T, int FMT> struct LaneQ {
             Elem<float>::unpack(v[0], v[1], q);
             Elem<float>::unpack(v[2], v[3], q + 8);
         }
+    }
+    __device__ __forceinline__ bool large() const
+    {
+        float top = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(q[i]));            // (a NaN is one either way)
+        return top > __uint_as_float(LARGE_Q);
     }
     __device__ __forceinline__ float dot(const uint4& w, uint32_t byte) const
     {
@@ -247,11 +260,35 @@ template <typename T, int FMT> struct LaneQ {
         }
         return d;
     }
+    __device__ __forceinline__ float dot_large(const uint4& w, uint32_t byte) const
+    {
+        const uint32_t words[4] = { w.x, w.y, w.z, w.w };
+        const float scale = scale_value(byte);
+        float d = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float k[4];
+            decode4<FMT>(words[i], k);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) d = fmaf(q[4 * i + x], k[x] * scale, d);
+        }
+        return d;
+    }
 };
 template <> struct LaneQ<bf16_t, DG4_KV_E4M3> {
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    static constexpr bool SHORT = true;
     uint4 a, b;
     __device__ __forceinline__ void load(const bf16_t* p) { a = ((const uint4*)p)[0]; b = ((const uint4*)p)[1]; }
+    __device__ __forceinline__ bool large() const
+    {
+        typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+        const uint32_t words[8] = { a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w };
+        u16x2 top = { 0, 0 };
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, words[i] & 0x7FFF7FFFu));
+        return max(top.x, top.y) > (LARGE_Q >> 16);
+    }
     __device__ __forceinline__ float dot(const uint4& w, uint32_t byte) const
     {
         const float scale = __uint_as_float(byte << 23);
@@ -261,6 +298,20 @@ template <> struct LaneQ<bf16_t, DG4_KV_E4M3> {
             d = __builtin_amdgcn_fdot2_f32_bf16(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, true), __builtin_bit_cast(bf16x2, q1), d, false);
         };
         four(w.x, a.x, a.y); four(w.y, a.z, a.w); four(w.z, b.x, b.y); four(w.w, b.z, b.w);
+        return d;
+    }
+    __device__ __forceinline__ float dot_large(const uint4& w, uint32_t byte) const
+    {
+        const uint32_t codes[4] = { w.x, w.y, w.z, w.w }, words[8] = { a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w };
+        float d = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float k[4];
+            decode4_scaled<DG4_KV_E4M3>(codes[i], byte, k);
+            uint32_t q0 = words[2 * i], q1 = words[2 * i + 1];
+            __asm__ volatile("" : "+v"(q0), "+v"(q1));         // (unpacked here and not, for every row, ahead of the loop)
+            d = fmaf(bf16_hi(q1), k[3], fmaf(bf16_lo(q1), k[2], fmaf(bf16_hi(q0), k[1], fmaf(bf16_lo(q0), k[0], d))));
+        }
         return d;
     }
 };
@@ -273,13 +324,13 @@ template <> struct LaneQ<bf16_t, DG4_KV_E4M3> {
 // addressing are 32 bits: FAR, for larger stores, has addresses of 64 bits and reads zeros from memory for them.
 // Up to eight entries a row are two groups of four (2,4: one group of eight 504 us for a million two-hop rows of bfloat16 at 256,
 // two of four 491 us, before the rows were grouped by XCD), up to sixteen two of eight; longer rows have a whole wave, whose groups
-// keep their loads in flight (15,135 rows of eight-hop cones of bfloat16 at 128: 58.6 us, 61.6 where each step moves on to its maximum).
+// keep their loads in flight (15,135 rows of eight-hop cones of bfloat16 at 128: 59.8 us, 3 more where each step moves on to its maximum).
 // Measured: 450 us for that million rows, 2.34 GB fetched and 0.51 written (6.3 TB/s) where the store, Q, the table and A are 1.6 GB:
 // bound by sources that several XCDs fetch. Long rows are bound by vector instructions (busy 89 % of the cycles), 64
 // for an entry in bfloat16 / e4m3: 16 conversions, 8 and 16 products, and what finds, scales and weighs it. 20,256 rows of fp32 at 128,
 // int8: 8.3 us. One row: 2.5 us, three waits of memory after one another.
 template <typename T, int FMT, int D, int S, int CH, bool ONCE, bool FAR>
-__global__ __launch_bounds__(256) void kv8_attn_kernel(dg4_kv8_attn_args p)
+__global__ __launch_bounds__(256, !ONCE && sizeof(T) == 2 && FMT == DG4_KV_E4M3 ? 5 : 1) void kv8_attn_kernel(dg4_kv8_attn_args p)
 {
     constexpr int LPR = D / 16, HEADS = D / 32, GPW = 64 / LPR;
     constexpr int RPW = GPW / S;                  // rows per wave
@@ -309,6 +360,11 @@ __global__ __launch_bounds__(256) void kv8_attn_kernel(dg4_kv8_attn_args p)
     entries(part * CH);
     LaneQ<T, FMT> q;
     q.load((const T*)p.q + r * D + sub * 16);
+    bool large = false;                           // the same for all lanes of the row, so that a row does not see its neighbours
+    if constexpr (LaneQ<T, FMT>::SHORT) {
+        constexpr int LANES = LPR * S;
+        large = (__ballot(q.large()) >> (lane / LANES * LANES) & (~0ull >> (64 - LANES))) != 0;
+    }
     const float c = 0.17677669529663687f;         // 1/sqrt(32)
     const float log2e = 1.4426950408889634f;      // (not taken into the scores: the lowest bias times this is no number)
     float m = -INFINITY, z = 0.f;
@@ -317,73 +373,93 @@ __global__ __launch_bounds__(256) void kv8_attn_kernel(dg4_kv8_attn_args p)
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[i] = 0.f;
     }
-    for (int c0 = part * CH; ONCE || c0 < p.ell_w; c0 += S * CH) {
-        if (!ONCE && ent[0].x == DG4_ELL_PAD) break;           // padding stands at the end only; the same for all lanes of the group
-        uint4 kw[CH], vw[CH];
-        uint32_t sw[CH];                          // scales: of K, and of V from bit 8
-        float b[CH];
+    // (A long row has the wave to itself and goes one way throughout: the choice inside the loop costs 15,135 rows of bfloat16 at 128
+    // 62.4 us instead of 59.8. The registers of five waves to a SIMD hold the ordinary way; the other spills a few.)
+    constexpr int SHORT_FORM = 0, LARGE = 1, BY_ROW = 2;
+    auto walk = [&](auto way_) __attribute__((always_inline)) {
+        constexpr int way = way_;
+        for (int c0 = part * CH; ONCE || c0 < p.ell_w; c0 += S * CH) {
+            if (!ONCE && ent[0].x == DG4_ELL_PAD) break;           // padding stands at the end only; the same for all lanes of the group
+            uint4 kw[CH], vw[CH];
+            uint32_t sw[CH];                          // scales: of K, and of V from bit 8
+            float b[CH];
 #pragma unroll
-        for (int j = 0; j < CH; ++j) {
-            const uint32_t e = j % 4 == 0 ? ent[j / 4].x : j % 4 == 1 ? ent[j / 4].y : j % 4 == 2 ? ent[j / 4].z : ent[j / 4].w;
-            const float bj = bias[head][e >> 30];
-            b[j] = e == DG4_ELL_PAD ? -INFINITY : bj;
-            const bool none = b[j] == -INFINITY;
-            if constexpr (FAR) {
-                const int64_t row = e & 0x3FFFFFFFu;
-                const uint8_t* at = none ? nothing : p.codes + row * (2 * D);
-                sw[j] = *(const uint16_t*)((none ? nothing : p.scales + row * (2 * HEADS)) + head * 2);
-                kw[j] = *(const uint4*)(at + sub * 16);
-                vw[j] = *(const uint4*)(at + D + sub * 16);
-            } else {
-                const uint32_t row = none ? NONE : e & 0x3FFFFFFFu;
-                const int at = (int)(row * (2 * D) + sub * 16);
-                sw[j] = dg4_raw_buffer_load2(scale_bytes, (int)(row * (2 * HEADS) + head * 2), 0, 0);
-                kw[j] = __builtin_bit_cast(uint4, dg4_raw_buffer_load16(code_bytes, at, 0, 0));
-                vw[j] = __builtin_bit_cast(uint4, dg4_raw_buffer_load16(code_bytes, at + D, 0, 0));
+            for (int j = 0; j < CH; ++j) {
+                const uint32_t e = j % 4 == 0 ? ent[j / 4].x : j % 4 == 1 ? ent[j / 4].y : j % 4 == 2 ? ent[j / 4].z : ent[j / 4].w;
+                const float bj = bias[head][e >> 30];
+                b[j] = e == DG4_ELL_PAD ? -INFINITY : bj;
+                const bool none = b[j] == -INFINITY;
+                if constexpr (FAR) {
+                    const int64_t row = e & 0x3FFFFFFFu;
+                    const uint8_t* at = none ? nothing : p.codes + row * (2 * D);
+                    sw[j] = *(const uint16_t*)((none ? nothing : p.scales + row * (2 * HEADS)) + head * 2);
+                    kw[j] = *(const uint4*)(at + sub * 16);
+                    vw[j] = *(const uint4*)(at + D + sub * 16);
+                } else {
+                    const uint32_t row = none ? NONE : e & 0x3FFFFFFFu;
+                    const int at = (int)(row * (2 * D) + sub * 16);
+                    sw[j] = dg4_raw_buffer_load2(scale_bytes, (int)(row * (2 * HEADS) + head * 2), 0, 0);
+                    kw[j] = __builtin_bit_cast(uint4, dg4_raw_buffer_load16(code_bytes, at, 0, 0));
+                    vw[j] = __builtin_bit_cast(uint4, dg4_raw_buffer_load16(code_bytes, at + D, 0, 0));
+                }
             }
-        }
-        if constexpr (!ONCE) entries(c0 + S * CH);             // the next step's entries travel with this step's rows
-        float s[CH];
-        float cm = m;
+            if constexpr (!ONCE) entries(c0 + S * CH);             // the next step's entries travel with this step's rows
+            float s[CH];
+            float cm = m;
+            auto score = [&](int j, float dot, float factor) __attribute__((always_inline)) {
+                dot += xor1(dot);
+                // (zeros times a q that is not finite are NaN: an entry that is none has no product)
+                dot = b[j] == -INFINITY ? 0.f : dot;
+                s[j] = fmaf(dot, factor, b[j]);
+                cm = fmaxf(cm, s[j]);
+            };
+            if (way == SHORT_FORM || (way == BY_ROW && !large)) {
 #pragma unroll
-        for (int j = 0; j < CH; ++j) {
-            float dot = q.dot(kw[j], sw[j] & 255u);
-            dot += xor1(dot);
-            // (zeros times a q that is not finite are NaN: an entry that is none has no product)
-            dot = b[j] == -INFINITY ? 0.f : dot;
-            s[j] = fmaf(dot, FMT == DG4_KV_E4M3 ? c : scale_value(sw[j] & 255u) * c, b[j]);
-            cm = fmaxf(cm, s[j]);
-        }
-        // What weights are relative to: the maximum; in a wave with steps to come (one row) what it was when some lane's last was more
-        // than 4 past it, so that few steps have sums to scale down. e^4 < 2^6, which every weight there is divided by: no sum of V is
-        // larger than it would be, and a source alone in its row still leaves as it is.
-        // (Nothing so far, -inf: any finite base will do, every weight is 0.)
-        if constexpr (ONCE) {
-            m = cm;
-        } else if (__any(cm > m + 4.f)) {
-            const float corr = __builtin_amdgcn_exp2f((m - (cm == -INFINITY ? 0.f : cm)) * log2e);
-            m = cm;
-            z *= corr;
+                for (int j = 0; j < CH; ++j) score(j, q.dot(kw[j], sw[j] & 255u), FMT == DG4_KV_E4M3 ? c : scale_value(sw[j] & 255u) * c);
+            } else if constexpr (LaneQ<T, FMT>::SHORT) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) acc[i] *= corr;
-        }
-        const float base = m == -INFINITY ? 0.f : m;
-#pragma unroll
-        for (int j = 0; j < CH; ++j) {
-            const float pj = __builtin_amdgcn_exp2f(ONCE ? (s[j] - base) * log2e : fmaf(s[j] - base, log2e, -6.f));
-            z += pj;
-            const float pv = FMT == DG4_KV_E4M3 ? pj : pj * scale_value(sw[j] >> 8);
-            const uint32_t words[4] = { vw[j].x, vw[j].y, vw[j].z, vw[j].w };
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float x[4];
-                decode4_scaled<FMT>(words[i], sw[j] >> 8, x);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) acc[4 * i + k] = ONCE && j == 0 ? pv * x[k] : fmaf(pv, x[k], acc[4 * i + k]);
+                for (int j = 0; j < CH; ++j) {
+                    // (taken as others than the words above, or what both ways share is kept in registers from before the branch)
+                    uint4 w = kw[j];
+                    __asm__ volatile("" : "+v"(w.x), "+v"(w.y), "+v"(w.z), "+v"(w.w));
+                    score(j, q.dot_large(w, sw[j] & 255u), c);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
+            // What weights are relative to: the maximum; in a wave with steps to come (one row) what it was when some lane's last was more
+            // than 4 past it, so that few steps have sums to scale down. e^4 < 2^6, which every weight there is divided by: no sum of V is
+            // larger than it would be, and a source alone in its row still leaves as it is.
+            // (Nothing so far, -inf: any finite base will do, every weight is 0.)
+            if constexpr (ONCE) {
+                m = cm;
+            } else if (__any(cm > m + 4.f)) {
+                const float corr = __builtin_amdgcn_exp2f((m - (cm == -INFINITY ? 0.f : cm)) * log2e);
+                m = cm;
+                z *= corr;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[i] *= corr;
+            }
+            const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll
+            for (int j = 0; j < CH; ++j) {
+                const float pj = __builtin_amdgcn_exp2f(ONCE ? (s[j] - base) * log2e : fmaf(s[j] - base, log2e, -6.f));
+                z += pj;
+                const float pv = FMT == DG4_KV_E4M3 ? pj : pj * scale_value(sw[j] >> 8);
+                const uint32_t words[4] = { vw[j].x, vw[j].y, vw[j].z, vw[j].w };
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float x[4];
+                    decode4_scaled<FMT>(words[i], sw[j] >> 8, x);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) acc[4 * i + k] = ONCE && j == 0 ? pv * x[k] : fmaf(pv, x[k], acc[4 * i + k]);
+                }
+            }
+            if constexpr (ONCE) break;
         }
-        if constexpr (ONCE) break;
-    }
+    };
+    if constexpr (ONCE || !LaneQ<T, FMT>::SHORT) walk(std::integral_constant<int, BY_ROW>{});
+    else if (large) walk(std::integral_constant<int, LARGE>{});
+    else walk(std::integral_constant<int, SHORT_FORM>{});
     // join the groups of the row: one maximum, then sums, each exchange leaving a lane half the features it had
     constexpr int KEPT = 16 / S;
     int first = 0;

@@ -42,3 +42,25 @@ def test_a_head_without_sources_gives_zeros_whatever_q_holds(fmt, hidden, dtype,
     assert B[1::4, 64:].isnan().all() and B[1::4][~single[1::4]][:, 32:64].isnan().all()
     want, bound = reference(g, range(0, n, 4), finite[::4], codes, scales, fmt, bias, dtype)
     assert (np.abs(to_np(B[::4]) - want) <= bound).all()
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("hops", [2, 5])
+@pytest.mark.parametrize("small", [-118, -124, -127, -131])
+def test_large_q_against_the_smallest_values(fmt, dtype, hops, small):
+    """K of 2^small, at the end of a float's range, against Q of about its reciprocal: ordinary scores."""
+    n, hidden = 90, 128
+    print(f"kv8 large Q {fmt} {dtype} hops={hops} K about 2^{small}", flush=True)
+    g = circuit(n, 30, hops, seed=4)
+    codes, scales = store(6, n, hidden, fmt)
+    rng = np.random.default_rng(11)
+    K = torch.from_numpy((rng.standard_normal((n, hidden)) * 2.0 ** small).astype(np.float32)).cuda()
+    V = torch.from_numpy(rng.standard_normal((n, hidden)).astype(np.float32)).cuda()
+    dg4.dg4_kv8_write(cfg(hidden, "f32"), fmt, K, V, codes, scales)
+    Q = torch.from_numpy(rng.standard_normal((n, hidden)) * 2.0 ** min(-small, 125)).to(tdtype(dtype)).cuda()
+    bias = torch.from_numpy(rng.standard_normal((4, 4)).astype(np.float32)).cuda()
+    want, bound = reference(g, range(n), Q, codes, scales, fmt, bias, dtype)
+    # (what a product below 2^-126 may lose against a score: 32 times 2^-149, nothing)
+    A = torch.full_like(Q, 7.0)
+    dg4.dg4_sparse_attn_kv8_fwd(cfg(hidden, dtype, hops), fmt, g, Q, codes, scales, bias, A)
+    err = np.abs(to_np(A) - want)
+    assert (err <= bound).all(), (err / bound).max()
