@@ -90,10 +90,13 @@ bool heads_config(const dg4_layer_cfg* c)
 // gates per level of the circuit's own, this kernel against launches: 199 and 176 us; three levels for each 203 and 406,
 // twenty 208 and 2168.
 // One layer over two hops in bf16 / 256 without feed-forward has a kernel of its own.
+// The kernel reads sources through structured buffers, one for each head: 256 bytes a gate in fp32, 128 in bf16. Circuits past
+// 2^24 (2^25) gates, whose rows such a buffer does not reach, take the other paths.
 bool heads_route(const dg4_layer_cfg* c, const dg4_graph* g)
 {
     // (without marks the nodes are copies in many shallow components: never narrow)
     if ((c->flags & DG4_PER_LEVEL) || !g->marks || !heads_config(c)) return false;
+    if (g->n * (int64_t)(64 * elt_size(c->dtype)) > DG4_ROW_BUFFER_BYTES) return false;
     const bool ffn = (c->flags & DG4_FFN) != 0;
     const bool streamed = dg4_flow_supports(c->dtype, c->hidden, 8) && (!ffn || c->hops <= 3);
     return dg4_dependency_width(g) <= (int64_t)dg4_head_groups(c->heads) * DG4_HEADS_ROWS * (!streamed ? 4 : c->hops >= 6 ? 2 : 1);
@@ -498,7 +501,11 @@ extern "C" int dg4_layer_fwd(const dg4_layer_cfg* cfg, dg4_graph* g, const void*
     const bool forced_levels = (cfg->flags & (DG4_PER_LEVEL | DG4_BOUNDED_KV)) != 0;
     const bool heads = heads_route(cfg, g);
     const bool resident = !heads && dt == DG4_BF16 && d == 256 && L == 1 && cfg->hops <= 2 && !forced_levels && (!ffn || whole_range);
-    const bool flow = !heads && !resident && !forced_levels && dg4_flow_supports(dt, d, g->ell_w) && (!ffn || g->ell_w <= 16);
+    // (rows of more than 8 entries are read there through a structured buffer over a layer's K|V store, 1 KB a gate: past 2^22 gates
+    // they go level by level. 4.5 M gates, 45,000 to a level: bf16 / 256, three hops, two layers 38 ms, where the kernel would take 26;
+    // fp32 / 128, one layer 19, 18; bf16 / 256, four hops, one layer 24, 24)
+    const bool reached = g->ell_w <= 8 || g->n * 2 * d * es <= DG4_ROW_BUFFER_BYTES;
+    const bool flow = !heads && !resident && !forced_levels && dg4_flow_supports(dt, d, g->ell_w) && (!ffn || g->ell_w <= 16) && reached;
     // a caller that has not changed the weights since its last call with this configuration, graph
     // and workspace vouches for the packed copies that call left behind
     const bool pack = !(cfg->flags & DG4_WEIGHTS_PACKED);

@@ -289,6 +289,9 @@ struct dg4_flow_args {
     float ln_eps; int epilogue; int project_kv;
     uint32_t spin_limit;
 };
+// Largest table that kernels read as a structured buffer (row_buffer): its index times its stride is a number of 32 bits, and rows
+// past it read others. The routes of dg4_layer_fwd keep such kernels to it.
+constexpr int64_t DG4_ROW_BUFFER_BYTES = (int64_t)1 << 32;
 bool dg4_flow_supports(int dtype, int hidden, int ell_w);
 int dg4_launch_pack_wa(int dtype, int hidden, const void* w, int ld, int col0, int n_cols, void* packed, hipStream_t s);
 int dg4_launch_flow(int dtype, int hidden, const dg4_flow_args& a, hipStream_t s);

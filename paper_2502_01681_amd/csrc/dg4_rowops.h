@@ -125,7 +125,8 @@ __device__ __forceinline__ void attend_core(const uint32_t (&ent)[W], const T* q
 // A table of rows in global memory as a structured buffer: row i at base + i * row_bytes, rows_total
 // rows. A load through it takes a row index and a byte offset inside the row; an index at or past
 // rows_total reads as zeros and costs no memory request (the range check of buffer addressing), which
-// is how a lane skips a row without a branch.
+// is how a lane skips a row without a branch. Index times stride is formed in 32 bits: the table holds at most
+// DG4_ROW_BUFFER_BYTES.
 typedef int dg4_i32x4 __attribute__((ext_vector_type(4)));
 __device__ dg4_i32x4 dg4_struct_buffer_load16(dg4_i32x4 rsrc, int vindex, int voffset, int soffset, int aux)
     __asm("llvm.amdgcn.struct.buffer.load.v4i32");
