@@ -365,8 +365,9 @@ def _call(where: str, cfg: LayerConfig, first):
     global _types, _raw_stream, _device
     if _types is None:
         import torch
-        _types = {"f32": torch.float32, "bf16": torch.bfloat16, "ids": torch.int32, "bytes": torch.uint8}
         _raw_stream, _device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+        # (last: another thread's first call goes by this one)
+        _types = {"f32": torch.float32, "bf16": torch.bfloat16, "ids": torch.int32, "bytes": torch.uint8}
     dev = first.get_device()
     if cfg.dtype not in ("f32", "bf16") or dev < 0 or dev != _device():
         raise DG4Error(-1, where)
