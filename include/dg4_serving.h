@@ -33,8 +33,9 @@ typedef enum {
  * reads as NaN.
  *   dg4_kv8_write: rows [row_begin, row_end) of K and V [*, hidden] (cfg->dtype) into the store; row r
  *   goes to store row ids[r], or to row r without ids (then row_end <= n_store). Entries of ids outside
- *   [0, n_store) are skipped (-1: a padded row); the others are distinct, and which of two rows with
- *   one id remains is not defined. Store rows that are not named stay as they are.
+ *   [0, n_store) are skipped (-1: a padded row). The others are to be distinct: a store row that is named
+ *   twice holds parts of both rows afterwards, codes of one under scales of the other among them, and
+ *   has to be written again. Store rows that are not named stay as they are.
  */
 int dg4_kv8_write(const dg4_layer_cfg* cfg, int32_t format, const void* K, const void* V,
                   int64_t row_begin, int64_t row_end, const int32_t* ids /* nullable, device */,

@@ -456,7 +456,8 @@ def _store_call(where: str, cfg: LayerConfig, fmt: str, codes, scales, ids, x, y
 
 def dg4_kv8_write(cfg: LayerConfig, fmt: str, K, V, codes, scales, ids=None, row_begin=0, row_end=None):
     """Rows [row_begin,row_end) of K and V into the 8-bit store (fmt "e4m3" | "int8"): codes uint8 [n, 2*hidden] and
-    scales uint8 [n, heads, 2] in place. ids: int32 store row of each row (outside the store: skipped), else the row itself."""
+    scales uint8 [n, heads, 2] in place. ids: int32 store row of each row (outside the store: skipped), else the row itself;
+    a store row that is named twice holds neither row whole."""
     f, row_end, n, ip, stream = _store_call("dg4_kv8_write", cfg, fmt, codes, scales, ids, K, V, row_begin, row_end)
     if f is None:
         return

@@ -64,3 +64,34 @@ def test_large_q_against_the_smallest_values(fmt, dtype, hops, small):
     dg4.dg4_sparse_attn_kv8_fwd(cfg(hidden, dtype, hops), fmt, g, Q, codes, scales, bias, A)
     err = np.abs(to_np(A) - want)
     assert (err <= bound).all(), (err / bound).max()
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("hidden,dtype", [(128, "f32"), (256, "bf16")])
+def test_a_store_row_named_twice_harms_no_other(fmt, hidden, dtype):
+    """What it holds itself is of the two rows that name it, byte by byte; written again, it is right."""
+    n, rows = 60, 50
+    rng = np.random.default_rng(3)
+    ids = rng.permutation(n)[:rows].astype(np.int32)
+    ids[[7, 30, 41]] = ids[[8, 12, 49]]
+    K, V = (torch.from_numpy(rng.standard_normal((rows, hidden)).astype(np.float32) * np.exp2(rng.integers(-9, 9, (rows, 1)))).to(tdtype(dtype)).cuda() for _ in range(2))
+
+    def written(k, v, at):
+        codes = torch.full((n, 2 * hidden), 0x55, dtype=torch.uint8, device="cuda")
+        scales = torch.full((n, hidden // 32, 2), 0x66, dtype=torch.uint8, device="cuda")
+        dg4.dg4_kv8_write(cfg(hidden, dtype), fmt, k, v, codes, scales, ids=torch.from_numpy(at).cuda())
+        return codes, scales
+    both = written(K, V, ids)
+    keep = np.ones(rows, dtype=bool)
+    keep[[7, 30, 41]] = False
+    last = written(K[torch.from_numpy(keep).cuda()].contiguous(), V[torch.from_numpy(keep).cuda()].contiguous(), ids[keep])
+    twice = ids[[8, 12, 49]]
+    keep[[7, 30, 41]], keep[[8, 12, 49]] = True, False
+    first = written(K[torch.from_numpy(keep).cuda()].contiguous(), V[torch.from_numpy(keep).cuda()].contiguous(), ids[keep])
+    others = torch.from_numpy(np.setdiff1d(np.arange(n), twice)).cuda()
+    for x, y, z in zip(both, last, first):
+        assert torch.equal(x[others], y[others])
+        assert ((x == y) | (x == z)).all()
+    again = torch.tensor([8, 12, 49], device="cuda")
+    dg4.dg4_kv8_write(cfg(hidden, dtype), fmt, K[again].contiguous(), V[again].contiguous(), *both, ids=torch.from_numpy(twice).cuda())
+    assert all(torch.equal(x, y) for x, y in zip(both, last))
