@@ -663,10 +663,11 @@ int launch_pack(const dg4_lora_pack_args& a, hipStream_t s)
     return hipGetLastError();
 }
 
-// (64 KB need no leave)
-template <typename K> int allow_lds(K kernel, int bytes)
+// (64 KB need no leave. It is given for the largest rank, so that a call of a smaller one in another thread takes none of it away
+// between this and the launch.)
+template <typename K> int allow_lds(K kernel, int bytes, int most)
 {
-    return bytes <= 65536 ? hipSuccess : hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    return bytes <= 65536 ? hipSuccess : hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, most);
 }
 
 template <typename T, int D>
@@ -679,14 +680,14 @@ int launch_proj(dg4_lora_args a, hipStream_t s)
         a.tile_rows = 1;
         while (a.tile_rows < ROWS && rows * (3 * D / 128) > (int64_t)512 * a.tile_rows) a.tile_rows *= 2;
         const int smem = StreamLds<T, D>::bytes(a.rank8);
-        if (const int e = allow_lds(kernel, smem); e != hipSuccess) return e;
+        if (const int e = allow_lds(kernel, smem, StreamLds<T, D>::bytes(DG4_MAX_RANK)); e != hipSuccess) return e;
         hipLaunchKernelGGL(kernel, dim3((unsigned)((rows + a.tile_rows - 1) / a.tile_rows), 3 * D / 128), dim3(256), smem, s, a);
     } else if constexpr (sizeof(T) == 2) {
         constexpr int PARTS = D == 256 ? 3 : 1;
         using L = WalkLds<D, 3 * D / 128 / PARTS>;
         const auto kernel = lora_resident_kernel<D, PARTS>;
         const int smem = L::bytes(a.rank8);
-        if (const int e = allow_lds(kernel, smem); e != hipSuccess) return e;
+        if (const int e = allow_lds(kernel, smem, L::bytes(DG4_MAX_RANK)); e != hipSuccess) return e;
         int dev = 0, cus = 0;
         if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess) return hipErrorInvalidDevice;
         // one workgroup per compute unit
@@ -695,7 +696,7 @@ int launch_proj(dg4_lora_args a, hipStream_t s)
     } else {
         const auto kernel = lora_stream_kernel<T, D, false>;
         const int smem = StreamLds<T, D>::bytes(a.rank8);
-        if (const int e = allow_lds(kernel, smem); e != hipSuccess) return e;
+        if (const int e = allow_lds(kernel, smem, StreamLds<T, D>::bytes(DG4_MAX_RANK)); e != hipSuccess) return e;
         hipLaunchKernelGGL(kernel, dim3((unsigned)((rows + ROWS - 1) / ROWS)), dim3(256), smem, s, a);
     }
     return hipGetLastError();

@@ -87,3 +87,33 @@ def test_products_at_the_end_of_the_range(hidden, dtype, rows):
     bound = (2.0 ** -16 if dtype == "bf16" else 0) * size + 2.0 ** -18 * size
     bound = bound.cpu() + (2.0 ** -24 if dtype == "f32" else 2.0 ** -8) * want.abs()
     assert ((got - want).abs() <= bound).all()
+
+
+def test_threads_with_adapters_of_different_ranks():
+    """Calls of the same kernel with little and with much shared memory, from two threads at once, on streams of their own."""
+    import threading
+    cfg = dg4.LayerConfig(256, 8, 2, 1, "bf16")
+    jobs = []
+    for rank in (1, 64):
+        packed = dg4.dg4_lora_pack(cfg, *weights(rank, 256, 2, rank, "bf16"))
+        S = rows_of(rank, 9_000, 256, "bf16")
+        adapter = (torch.arange(9_000, device="cuda") // 4_500).to(torch.int32)
+        jobs.append((packed, S, adapter, project(cfg, packed, S, adapter), [torch.zeros_like(S) for _ in range(3)]))
+    torch.cuda.synchronize()
+    failed = []
+
+    def work(packed, S, adapter, want, out):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(200):
+                    dg4.dg4_qkv_proj_lora(cfg, packed, S, adapter, *out)
+                torch.cuda.current_stream().synchronize()
+        except Exception as e:                     # (an assertion in a thread would be lost)
+            failed.append(e)
+    threads = [threading.Thread(target=work, args=job) for job in jobs]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed
+    assert all(torch.equal(x, y) for job in jobs for x, y in zip(job[3], job[4]))
