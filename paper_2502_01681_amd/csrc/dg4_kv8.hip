@@ -325,10 +325,11 @@ template <> struct LaneQ<bf16_t, DG4_KV_E4M3> {
 // Up to eight entries a row are two groups of four (2,4: one group of eight 504 us for a million two-hop rows of bfloat16 at 256,
 // two of four 491 us, before the rows were grouped by XCD), up to sixteen two of eight; longer rows have a whole wave, whose groups
 // keep their loads in flight (15,135 rows of eight-hop cones of bfloat16 at 128: 59.8 us, 3 more where each step moves on to its maximum).
-// Measured: 450 us for that million rows, 2.34 GB fetched and 0.51 written (6.3 TB/s) where the store, Q, the table and A are 1.6 GB:
-// bound by sources that several XCDs fetch. Long rows are bound by vector instructions (busy 89 % of the cycles), 64
-// for an entry in bfloat16 / e4m3: 16 conversions, 8 and 16 products, and what finds, scales and weighs it. 20,256 rows of fp32 at 128,
-// int8: 8.3 us. One row: 2.5 us, three waits of memory after one another.
+// Measured: 446 us for that million rows, 2.34 GB fetched and 0.51 written (6.4 TB/s) where the store, Q, the table and A are 1.6 GB:
+// bound by sources that several XCDs fetch. Long rows are bound by vector instructions, 70 for an entry in bfloat16 / e4m3: 16
+// conversions, 8 and 16 products, and what finds, scales and weighs it. Counted for those 15,135 rows: 29.9 M instructions, 119,000
+// cycles of each SIMD, 49 of the 60 us at 2.4 GHz. fp32 / int8 at 128: 84 us, bfloat16 / int8 at 256: 155, fp32 / e4m3 at 256: 116.
+// 20,256 short rows of fp32 at 128, int8: 8.9 us. One row: 2.7 us, three waits of memory after one another.
 template <typename T, int FMT, int D, int S, int CH, bool ONCE, bool FAR>
 __global__ __launch_bounds__(256, !ONCE && sizeof(T) == 2 && FMT == DG4_KV_E4M3 ? 5 : 1) void kv8_attn_kernel(dg4_kv8_attn_args p)
 {

@@ -40,7 +40,9 @@ __device__ __forceinline__ int column_of(int m) { return 16 * ((m >> 2) & 1) + 4
 // Calls with up to so many elements of S split the columns over workgroups. Measured, split | not split, in us, rank 16:
 // bfloat16 at hidden 256, 4000 rows 8.8 | 9.9, 8000 rows 12.7 | 13.5, 10,000 rows 15.8 | 14.0; at 128, 4000 rows 5.5 | 9.7,
 // 14,000 rows 8.9 | 9.8; fp32 at 256, 4000 rows 28.9 | 43.9, 8000 rows 44.6 | 41.3, 16,000 rows 78.6 | 64.9; at 128, 4000 rows
-// 11.7 | 15.0, 12,000 rows 21.5 | 22.4, 16,000 rows 24.7 | 22.9, 24,000 rows 34.3 | 30.7.
+// 11.7 | 15.0, 12,000 rows 21.5 | 22.4, 16,000 rows 24.7 | 22.9, 24,000 rows 34.3 | 30.7. Other ranks cross within a few per cent of the
+// same places: bfloat16 at 256, 8000 rows, rank 1 11.9 | 11.1, rank 64 17.4 | 18.2; fp32 at 128, 14,000 rows 22.3 | 21.0 and 34.2 | 35.8.
+// Rows with 16 adapters in any order: 8000 rows 34.8 | 44.9, 10,000 47.2 | 45.1; fp32 at 128, 14,000 rows 77.7 | 68.3.
 template <typename T> constexpr int64_t SPREAD_ELEMENTS = sizeof(T) == 2 ? 1 << 21 : 7 << 18;
 template <typename T> constexpr int PIECE = 16 / (int)sizeof(T);      // elements of 16 bytes
 inline int rank8(int rank) { return (rank + 7) / 8 * 8; }
@@ -433,10 +435,13 @@ template <int D, int JT> struct WalkLds {
 // multiply and store and wait for no load; U_a sits in LDS until the adapter changes. The other four, sixteen rows each, request
 // the rows two tiles ahead, put the next tile's into LDS and form their T, with D_a in registers until the adapter changes. One
 // barrier per tile. A tile whose rows differ in their adapter goes half by half, U_a of one adapter after the other.
-// Measured, rank 16, a million rows of 200 circuits at hidden 256: 634 us, 0.67 PFLOP/s and 3.2 TB/s; the multiplying waves bind it,
-// one to each SIMD, 2900 cycles of S W (the matrix cores: 2050), 850 of T U and 2600 to hand a tile to the memory, one after the other.
-// Without the stores 500 us; two workgroups of four waves to a compute unit instead 680 us; rows in registers and W from the L2
-// 654 us. 500,000 rows at 128: 127 us, 4.1 TB/s. 200,000 rows at 256 with 16 adapters in any order 637 us, in runs 105 us.
+// Measured, rank 16, a million rows of 40 circuits with 16 adapters at hidden 256: 631 us (of 200 circuits 662: most tiles at a change
+// of adapter are mixed), 0.68 PFLOP/s and 3.3 TB/s; the multiplying waves bind it, one to each SIMD, 2900 cycles of S W (the matrix
+// cores: 2050), 850 of T U and 2600 to hand a tile to the memory, one after the other. Without the stores 500 us; two workgroups of four
+// waves to a compute unit instead 680 us; rows in registers and W from the L2 654 us. 500,000 rows at 128: 121 us, 4.2 TB/s.
+// Adapters in any order, 200,000 rows: a tile forms T U of each of its adapters for all its rows. Of 4, 16 and 64 adapters at 256
+// 259, 647 and 1070 us (in runs 130 to 137), at 128 104, 271 and 461 (45 to 48); the streaming kernel, not split, 268, 633 and 1030,
+// at 128 99, 226 and 366, but 177 and 57 in runs.
 template <int D, int PARTS>
 __global__ __launch_bounds__(512, 2) void lora_resident_kernel(dg4_lora_args p)
 {
@@ -676,7 +681,9 @@ int launch_proj(dg4_lora_args a, hipStream_t s)
     const int64_t rows = a.row_end - a.row_begin;
     if (rows * D <= SPREAD_ELEMENTS<T>) {
         const auto kernel = lora_stream_kernel<T, D, true>;
-        // rows per tile: few enough for two workgroups per compute unit
+        // Rows per tile: few enough for two workgroups per compute unit. bfloat16 at 256, in us with 256, 512 and 1024 workgroups instead:
+        // 64 rows with an adapter each 5.6, 5.1 and 5.1 (tiles of 2 rows and of 1), 170 rows 7.8, 6.5, 7.5, 340 rows 11.3, 8.4, 10.1; rows of
+        // eight circuits in runs 4.5, 5.2, 5.1; 5.6, 6.3, 7.6; 5.6, 6.3, 8.6. fp32 at 128, 340 rows 11.1, 11.0, 15.3 and 8.1, 10.7, 15.3.
         a.tile_rows = 1;
         while (a.tile_rows < ROWS && rows * (3 * D / 128) > (int64_t)512 * a.tile_rows) a.tile_rows *= 2;
         const int smem = StreamLds<T, D>::bytes(a.rank8);
