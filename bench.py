@@ -187,11 +187,12 @@ def main():
             return "sweep_kernel (persistent, weights resident in registers)"
         streamed = (c.dtype, c.hidden) in (("f32", 128), ("bf16", 256)) and (not ffn or g.hops <= 3)
         gates_per_level = g.n // (depth or g.n_levels)
-        if gates_per_level <= 256 // c.heads * 16 * (4 if not streamed else 2 if g.hops >= 6 else 1):
+        es = 4 if c.dtype == "f32" else 2
+        if gates_per_level <= 256 // c.heads * 16 * (4 if not streamed else 2 if g.hops >= 6 else 1) and g.n * 64 * es <= 2 ** 32:
             return "heads_kernel (persistent, heads of a tile spread over compute units)"
         if c.dtype == "bf16" and c.hidden == 256 and c.n_layers == 1 and g.hops <= 2:
             return "sweep_kernel (persistent, weights resident in registers)"
-        if not streamed:
+        if not streamed or (g.hops > 2 and g.n * 2 * c.hidden * es > 2 ** 32):
             return "level-by-level launches"
         return "flow_kernel (persistent, weights streamed" + (", several lane groups per neighbour row)" if g.hops > 3 else ")")
 

@@ -328,8 +328,9 @@ int dg4_sparse_attn_fwd(const dg4_layer_cfg* cfg, dg4_graph* g, int64_t row_begi
  * The order in which a sweep over ALL levels visits the gates is the library's (dependency-driven
  * tiles in the persistent kernels, Eq. 1 levels in level-by-level launches) and does not change a
  * bit of the result; DG4_LEVEL_ORDER forces the graph's own levels (for comparisons).
- * Persistent sweeps (everything but DG4_PER_LEVEL, DG4_BOUNDED_KV and, on circuits with many gates per level,
- * DG4_FFN on rows wider than 16 entries and the shapes fp32 / 256 and bf16 / 128, which run level by level) hand
+ * Persistent sweeps (everything but DG4_PER_LEVEL, DG4_BOUNDED_KV and, on circuits with many gates per level or more
+ * than 2^24 gates (bf16 2^25), DG4_FFN on rows wider than 16 entries, the shapes fp32 / 256 and bf16 / 128, and rows wider
+ * than 8 entries on more than 2^22 gates, which run level by level) hand
  * tiles of gates to resident workgroups, which wait for the
  * tiles their gates read from. Any resident workgroup carries the sweep on; on circuits with few gates per
  * level a tile is worked on by one workgroup per head, and any `heads` resident workgroups do. Should such a wait

@@ -15,7 +15,9 @@ extern "C" {
 /* Element format of a K|V store in 8 bits (dg4_kv8_write) */
 typedef enum {
     DG4_KV_E4M3 = 0,        /* floating: 4 exponent and 3 mantissa bits, largest 448; relative  */
-                            /* error of a value at most 2^-4 down to 2^-14 of its block's range */
+                            /* error of a value at most 2^-4 down to 2^-13 of its block's       */
+                            /* largest magnitude, below that at most 2^-17 of the latter        */
+                            /* (2^-137 where scales end)                                        */
     DG4_KV_INT8 = 1         /* whole numbers -127 .. 127; error at most 1/127 of the block's    */
                             /* largest magnitude (or 2^-128), four times less on average than   */
                             /* e4m3's                                                           */

@@ -496,7 +496,7 @@ extern "C" int dg4_layer_fwd(const dg4_layer_cfg* cfg, dg4_graph* g, const void*
     // Which path: the kernel specialised for bf16 / hidden 256 / one layer / cones of two hops (weights
     // resident in registers), the persistent dataflow kernel for the other shapes and any number of
     // layers, or level-by-level launches (DG4_PER_LEVEL, DG4_BOUNDED_KV, the feed-forward sub-block
-    // on neighbour rows wider than 16 entries).
+    // on neighbour rows wider than 16 entries, stores past what the dataflow kernel's buffers reach).
     const bool whole_range = level_begin == 0 && level_end == (int32_t)g->max_level + 1;
     const bool forced_levels = (cfg->flags & (DG4_PER_LEVEL | DG4_BOUNDED_KV)) != 0;
     const bool heads = heads_route(cfg, g);
