@@ -34,6 +34,13 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi)
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2_t));
 }
 
+// Sixteen bytes to memory past the caches
+__device__ __forceinline__ void store_stream(void* p, const uint4& v)
+{
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), (u32x4*)p);
+}
+
 // Lane exchange inside a group of 4 lanes by data-parallel primitives.
 __device__ __forceinline__ float xor1(float v)   // lane ^ 1
 {

@@ -143,13 +143,6 @@ __global__ __launch_bounds__(256) void kv8_write_kernel(dg4_kv8_args p)
     }
 }
 
-// Results leave past the caches
-__device__ __forceinline__ void store_stream(void* p, const uint4& v)
-{
-    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-    __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), (u32x4*)p);
-}
-
 // A lane takes what it stores as 16 bytes, so that a wave's store is whole lines: four features of fp32, eight of bfloat16
 // (402,193 rows of fp32 at hidden 256, 1.04 GB moved: 250 us with two 16-byte stores a lane, of every other piece each, 155 us, 6.7
 // TB/s, so; 181 us where rows leave through the caches). U rows per lane: 185, 155 and 175 us with 1, 2 and 4.

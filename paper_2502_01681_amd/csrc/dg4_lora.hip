@@ -26,13 +26,6 @@
 
 namespace {
 
-// Results leave past the caches, which are the weights' (a million rows of bfloat16 at hidden 256: 641 us, through them 652)
-__device__ __forceinline__ void store_stream(void* p, const uint4& v)
-{
-    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-    __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), (u32x4*)p);
-}
-
 // Weights are the A operand of the 32x32 products and the rows the B operand, so that a lane's 16 accumulators belong to one
 // row; with column 16 hi + 4 a + b at operand row 8 a + 4 hi + b they are 16 neighbouring columns.
 __device__ __forceinline__ int column_of(int m) { return 16 * ((m >> 2) & 1) + 4 * (m >> 3) + (m & 3); }
@@ -266,7 +259,8 @@ struct Outputs {
 };
 
 // JT finished column tiles of the wave's rows, through its own corner of LDS (a wave's LDS operations complete in order), as
-// 16-byte pieces of rows to Q, K or V
+// 16-byte pieces of rows to Q, K or V, past the caches, which are the weights' (a million rows of bfloat16 at hidden 256: 641 us, through
+// them 652)
 template <typename T, int D, int JT, int STRIDE>
 __device__ __forceinline__ void put_tiles(const Outputs& to, const f32x16* acc, T* out_rows, int64_t r0, int64_t r_end, int tile, int lane)
 {
