@@ -138,6 +138,22 @@ def lib():
         L.dg4_kv8_read.argtypes = [ctypes.POINTER(_Cfg), _I32, _P, _P, _I64, _P, _I64, _I64, _P, _P, _P]
         L.dg4_sparse_attn_kv8_fwd.restype = ctypes.c_int
         L.dg4_sparse_attn_kv8_fwd.argtypes = [ctypes.POINTER(_Cfg), _I32, _P, _I64, _I64, _P, _P, _P, _P, _P, _P, _P]
+        L.dg4_kv4_write.restype = ctypes.c_int
+        L.dg4_kv4_write.argtypes = [ctypes.POINTER(_Cfg), _P, _P, _I64, _I64, _P, _P, _P, _I64, _P]
+        L.dg4_kv4_read.restype = ctypes.c_int
+        L.dg4_kv4_read.argtypes = [ctypes.POINTER(_Cfg), _P, _P, _I64, _P, _I64, _I64, _P, _P, _P]
+        L.dg4_sparse_attn_kv4_fwd.restype = ctypes.c_int
+        L.dg4_sparse_attn_kv4_fwd.argtypes = [ctypes.POINTER(_Cfg), _P, _I64, _I64, _P, _P, _P, _P, _P, _P, _P]
+        L.dg4_mx4_packed_bytes.restype = _I64
+        L.dg4_mx4_packed_bytes.argtypes = [ctypes.POINTER(_Cfg), _I32, _I32]
+        L.dg4_mx4_pack.restype = ctypes.c_int
+        L.dg4_mx4_pack.argtypes = [ctypes.POINTER(_Cfg), _P, _I32, _I32, _P, _I64, _P]
+        L.dg4_qkv_proj_mx4.restype = ctypes.c_int
+        L.dg4_qkv_proj_mx4.argtypes = [ctypes.POINTER(_Cfg), _P, _I64, _P, _I64, _I64, _P, _P, _P, _P]
+        L.dg4_qkv_proj_kv4.restype = ctypes.c_int
+        L.dg4_qkv_proj_kv4.argtypes = [ctypes.POINTER(_Cfg), _P, _I64, _P, _I64, _I64, _P, _P, _P, _P, _I64, _P]
+        L.dg4_ffn_mx4_fwd.restype = ctypes.c_int
+        L.dg4_ffn_mx4_fwd.argtypes = [ctypes.POINTER(_Cfg), _P, _I64, _P, _I64, _P, _I64, _I64, _P, _P]
         L.dg4_layer_fwd.restype = ctypes.c_int
         L.dg4_layer_fwd.argtypes = [ctypes.POINTER(_Cfg), _P, _P, ctypes.POINTER(_P), _I32, _I32, _P, _P, _I64, _P]
         L.dg4_sweep_elapsed_ms.restype = ctypes.c_int
@@ -374,9 +390,9 @@ def _call(where: str, cfg: LayerConfig, first):
     return _types[cfg.dtype], dev, _raw_stream(dev)
 
 
-def _shape(cfg: LayerConfig):
+def _shape(cfg: LayerConfig, ln_eps=0.0):
     """What the serving calls look at of a configuration, for the C call (its flags are dg4_layer_fwd's)."""
-    return ctypes.byref(_Cfg(cfg.hidden, cfg.heads, cfg.hops, 1, DG4_F32 if cfg.dtype == "f32" else DG4_BF16))
+    return ctypes.byref(_Cfg(cfg.hidden, cfg.heads, cfg.hops, 1, DG4_F32 if cfg.dtype == "f32" else DG4_BF16, 0, ln_eps))
 
 
 @dataclass
@@ -435,15 +451,20 @@ def dg4_qkv_proj_lora(cfg: LayerConfig, weights: LoraWeights, S, adapter, Q, K, 
     _check(rc, where)
 
 
-def _store_call(where: str, cfg: LayerConfig, fmt: str, codes, scales, ids, x, y, row_begin, row_end):
-    """What the calls on a K|V store in 8 bits check and fill in, for rows x and y beside it: (format or, with nothing to
+_IN_4_BITS = object()            # _store_call's fmt for a store in 4 bits
+
+
+def _store_call(where: str, cfg: LayerConfig, fmt, codes, scales, ids, x, y, row_begin, row_end):
+    """What the calls on a K|V store in 8 or 4 bits check and fill in, for rows x and y beside it: (format or, with nothing to
     do, None; end of the range; store rows; address of ids; stream)."""
     td, dev, stream = _call(where, cfg, codes)
     n, rows = codes.shape[0], x.shape[0]
     row_end = rows if row_end is None else row_end
+    four = fmt is _IN_4_BITS
     k, byte = rows * cfg.hidden, _types["bytes"]               # (_refused of each, without the calls: a level's call is short)
-    if (fmt not in KV_FORMATS or row_end > rows or x.dtype is not td or y.dtype is not td or codes.dtype is not byte or
-            scales.dtype is not byte or x.numel() != k or y.numel() != k or codes.numel() != n * 2 * cfg.hidden or
+    if (not (four or fmt in KV_FORMATS) or row_end > rows or x.dtype is not td or y.dtype is not td or codes.dtype is not byte or
+            scales.dtype is not byte or x.numel() != k or y.numel() != k or
+            codes.numel() != (n if four else 2 * n) * cfg.hidden or
             scales.shape != (n, cfg.heads, 2) or not (x.is_contiguous() and y.is_contiguous() and codes.is_contiguous() and
                                                       scales.is_contiguous()) or
             x.get_device() != dev or y.get_device() != dev or scales.get_device() != dev or
@@ -451,7 +472,7 @@ def _store_call(where: str, cfg: LayerConfig, fmt: str, codes, scales, ids, x, y
         raise DG4Error(-1, where)
     if row_begin == row_end == 0 or n == 0 and ids is not None:      # (an empty tensor has no address)
         return None, 0, n, None, stream
-    return KV_FORMATS[fmt], row_end, n, ids.data_ptr() if ids is not None else None, stream
+    return 4 if four else KV_FORMATS[fmt], row_end, n, ids.data_ptr() if ids is not None else None, stream
 
 
 def dg4_kv8_write(cfg: LayerConfig, fmt: str, K, V, codes, scales, ids=None, row_begin=0, row_end=None):
@@ -487,6 +508,120 @@ def dg4_sparse_attn_kv8_fwd(cfg: LayerConfig, fmt: str, g: Graph, Q, codes, scal
     rc = lib().dg4_sparse_attn_kv8_fwd(_shape(cfg), f, g.handle, row_begin, row_end, ip, Q.data_ptr(), codes.data_ptr(),
                                        scales.data_ptr(), rel_bias.data_ptr(), A.data_ptr(), stream)
     _check(rc, "dg4_sparse_attn_kv8_fwd")
+
+
+def dg4_kv4_write(cfg: LayerConfig, K, V, codes, scales, ids=None, row_begin=0, row_end=None):
+    """Rows [row_begin,row_end) of K and V into the store in 4 bits: codes uint8 [n, hidden] and scales uint8 [n, heads, 2] in
+    place. ids: int32 store row of each row (outside the store: skipped), else the row itself; a store row that is named twice
+    holds neither row whole."""
+    f, row_end, n, ip, stream = _store_call("dg4_kv4_write", cfg, _IN_4_BITS, codes, scales, ids, K, V, row_begin, row_end)
+    if f is None:
+        return
+    rc = lib().dg4_kv4_write(_shape(cfg), K.data_ptr(), V.data_ptr(), row_begin, row_end, ip, codes.data_ptr(),
+                             scales.data_ptr(), n, stream)
+    _check(rc, "dg4_kv4_write")
+
+
+def dg4_kv4_read(cfg: LayerConfig, codes, scales, K, V, ids=None, row_begin=0, row_end=None):
+    """Rows [row_begin,row_end) of K and V, in place, from the store in 4 bits; ids as in dg4_kv4_write."""
+    f, row_end, n, ip, stream = _store_call("dg4_kv4_read", cfg, _IN_4_BITS, codes, scales, ids, K, V, row_begin, row_end)
+    if f is None:
+        return
+    rc = lib().dg4_kv4_read(_shape(cfg), codes.data_ptr(), scales.data_ptr(), n, ip, row_begin, row_end,
+                            K.data_ptr(), V.data_ptr(), stream)
+    _check(rc, "dg4_kv4_read")
+
+
+def dg4_sparse_attn_kv4_fwd(cfg: LayerConfig, g: Graph, Q, codes, scales, rel_bias, A, ids=None, row_begin=0, row_end=None):
+    """Cone attention over the store in 4 bits (row = node id). ids: int32 gate of each row of Q and A, else the row itself."""
+    where = "dg4_sparse_attn_kv4_fwd"
+    f, row_end, n, ip, stream = _store_call(where, cfg, _IN_4_BITS, codes, scales, ids, Q, A, row_begin, row_end)
+    if n < g.n or _refused(rel_bias, _types["f32"], codes.get_device(), 4 * cfg.heads):
+        raise DG4Error(-1, where)
+    if f is None:
+        return
+    rc = lib().dg4_sparse_attn_kv4_fwd(_shape(cfg), g.handle, row_begin, row_end, ip, Q.data_ptr(), codes.data_ptr(),
+                                       scales.data_ptr(), rel_bias.data_ptr(), A.data_ptr(), stream)
+    _check(rc, where)
+
+
+@dataclass
+class Mx4Weights:
+    """A weight matrix [k, n] in blocks of 4 bits, in matrix-core operand order (dg4_mx4_pack); read only from then on."""
+    packed: object               # uint8 device tensor
+    k: int
+    n: int
+    hidden: int
+
+
+def dg4_mx4_packed_bytes(cfg: LayerConfig, k: int, n: int) -> int:
+    r = lib().dg4_mx4_packed_bytes(_shape(cfg), k, n)
+    if r < 0:
+        raise DG4Error(int(r), "dg4_mx4_packed_bytes")
+    return int(r)
+
+
+def dg4_mx4_pack(cfg: LayerConfig, W) -> Mx4Weights:
+    """W: Wqkv [hidden, 3*hidden], W1 [hidden, 4*hidden] or W2 [4*hidden, hidden]."""
+    where = "dg4_mx4_pack"
+    td, dev, stream = _call(where, cfg, W)
+    if W.dim() != 2 or _refused(W, td, dev, W.numel()):
+        raise DG4Error(-1, where)
+    k, n = W.shape
+    packed = _ws(dg4_mx4_packed_bytes(cfg, k, n), W)
+    rc = lib().dg4_mx4_pack(_shape(cfg), W.data_ptr(), k, n, packed.data_ptr(), packed.numel(), stream)
+    _check(rc, where)
+    return Mx4Weights(packed, k, n, cfg.hidden)
+
+
+def _mx4_refused(weights: Mx4Weights, cfg: LayerConfig, dev, k, n) -> bool:
+    return weights.hidden != cfg.hidden or weights.k != k or weights.n != n or weights.packed.get_device() != dev
+
+
+def dg4_qkv_proj_mx4(cfg: LayerConfig, weights: Mx4Weights, S, Q, K, V, row_begin=0, row_end=None):
+    """Q, K, V rows [row_begin,row_end) = S rows x Wqkv, both in blocks of 4 bits. In place."""
+    where, d, rows = "dg4_qkv_proj_mx4", cfg.hidden, S.shape[0]
+    td, dev, stream = _call(where, cfg, S)
+    row_end = rows if row_end is None else row_end
+    if (row_end > rows or _mx4_refused(weights, cfg, dev, d, 3 * d) or _refused(S, td, dev, rows * d) or
+            _refused(Q, td, dev, rows * d) or _refused(K, td, dev, rows * d) or _refused(V, td, dev, rows * d)):
+        raise DG4Error(-1, where)
+    if row_begin == row_end == 0:                # (an empty tensor has no address)
+        return
+    packed = weights.packed
+    rc = lib().dg4_qkv_proj_mx4(_shape(cfg), packed.data_ptr(), packed.numel(), S.data_ptr(), row_begin, row_end,
+                                Q.data_ptr(), K.data_ptr(), V.data_ptr(), stream)
+    _check(rc, where)
+
+
+def dg4_qkv_proj_kv4(cfg: LayerConfig, weights: Mx4Weights, S, Q, codes, scales, ids=None, row_begin=0, row_end=None):
+    """dg4_qkv_proj_mx4 with K and V straight into the store in 4 bits (codes, scales, ids as in dg4_kv4_write). In place."""
+    where, d = "dg4_qkv_proj_kv4", cfg.hidden
+    f, end, n, ip, stream = _store_call(where, cfg, _IN_4_BITS, codes, scales, ids, S, Q, row_begin, row_end)
+    # (a store without rows has no address, and rows of Q would have to be written all the same)
+    if _mx4_refused(weights, cfg, codes.get_device(), d, 3 * d) or f is None and n == 0 and S.shape[0]:
+        raise DG4Error(-1, where)
+    if f is None:
+        return
+    packed = weights.packed
+    rc = lib().dg4_qkv_proj_kv4(_shape(cfg), packed.data_ptr(), packed.numel(), S.data_ptr(), row_begin, end, ip,
+                                Q.data_ptr(), codes.data_ptr(), scales.data_ptr(), n, stream)
+    _check(rc, where)
+
+
+def dg4_ffn_mx4_fwd(cfg: LayerConfig, W1: Mx4Weights, W2: Mx4Weights, S, Out, row_begin=0, row_end=None):
+    """Out rows [row_begin,row_end) = LayerNorm(S + relu(S W1) W2), products in blocks of 4 bits. In place."""
+    where, d, rows = "dg4_ffn_mx4_fwd", cfg.hidden, S.shape[0]
+    td, dev, stream = _call(where, cfg, S)
+    row_end = rows if row_end is None else row_end
+    if (row_end > rows or _mx4_refused(W1, cfg, dev, d, 4 * d) or _mx4_refused(W2, cfg, dev, 4 * d, d) or
+            _refused(S, td, dev, rows * d) or _refused(Out, td, dev, rows * d)):
+        raise DG4Error(-1, where)
+    if row_begin == row_end == 0:                # (an empty tensor has no address)
+        return
+    rc = lib().dg4_ffn_mx4_fwd(_shape(cfg, cfg.ln_eps), W1.packed.data_ptr(), W1.packed.numel(), W2.packed.data_ptr(),
+                               W2.packed.numel(), S.data_ptr(), row_begin, row_end, Out.data_ptr(), stream)
+    _check(rc, where)
 
 
 def dg4_layer_fwd(cfg: LayerConfig, g: Graph, X, weights, Hout, level_begin=0, level_end=None, workspace=None):

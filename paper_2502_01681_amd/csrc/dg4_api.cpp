@@ -175,16 +175,56 @@ int check_lora(const dg4_layer_cfg* cfg, int32_t n_adapters, int32_t* rank)
     return *rank > DG4_MAX_RANK ? DG4_EUNSUPPORTED : DG4_OK;
 }
 
-// What the calls on a K|V store in 8 bits share: configuration, the store's two arrays, the range of rows
-int check_kv8(const dg4_layer_cfg* cfg, int32_t format, const int32_t* ids, const uint8_t* codes, const uint8_t* scales,
-              int64_t n_store, int64_t row_begin, int64_t row_end)
+// What the calls on a K|V store in 8 or 4 bits share: configuration, the store's two arrays, the range of rows
+int check_store(const dg4_layer_cfg* cfg, const int32_t* ids, const uint8_t* codes, const uint8_t* scales,
+                int64_t n_store, int64_t row_begin, int64_t row_end)
 {
     const int rc = check_cfg(cfg, false);
     if (rc != DG4_OK) return rc;
-    if (format != DG4_KV_E4M3 && format != DG4_KV_INT8) return DG4_EINVAL;
     if (!codes || !scales || !aligned16(codes, scales) || ((uintptr_t)ids & 3)) return DG4_EINVAL;
     if (n_store < 0 || row_begin < 0 || row_end < row_begin || (!ids && row_end > n_store)) return DG4_EINVAL;
     return DG4_OK;
+}
+int check_kv8(const dg4_layer_cfg* cfg, int32_t format, const int32_t* ids, const uint8_t* codes, const uint8_t* scales,
+              int64_t n_store, int64_t row_begin, int64_t row_end)
+{
+    const int rc = check_store(cfg, ids, codes, scales, n_store, row_begin, row_end);
+    if (rc != DG4_OK) return rc;
+    return format == DG4_KV_E4M3 || format == DG4_KV_INT8 ? (int)DG4_OK : (int)DG4_EINVAL;
+}
+
+// The rest of what attention over a store checks and fills in (*todo: whether there is a row to do)
+int attn_over_store(const dg4_layer_cfg* cfg, dg4_graph* g, int64_t row_begin, int64_t row_end, const int32_t* ids, const void* Q,
+                    const uint8_t* codes, const uint8_t* scales, const float* rel_bias, void* A, dg4_kv8_attn_args* a, bool* todo)
+{
+    *todo = false;
+    if (!Q || !rel_bias || !A || !aligned16(Q, A) || ((uintptr_t)rel_bias & 3) || g->hops != cfg->hops) return DG4_EINVAL;
+    if (row_end == row_begin || g->n == 0) return DG4_OK;
+    if (A != Q && overlap(cfg, A, Q, row_end - row_begin)) return DG4_EINVAL;
+    const int rc = dg4_graph_ensure_device(g);
+    if (rc != DG4_OK) return rc;
+    int dev = -1;
+    if (hipGetDevice(&dev) != hipSuccess) return DG4_EHIP;
+    if (dev != g->device) return DG4_EINVAL;
+    a->q = Q; a->a = A;
+    a->codes = codes; a->scales = scales; a->n = g->n;
+    a->rel_bias = rel_bias;
+    a->ell = g->d_ell_id; a->ell_w = g->ell_w;
+    a->ids = ids; a->row_begin = row_begin; a->row_end = row_end;
+    *todo = true;
+    return DG4_OK;
+}
+
+// What the calls with weights in 4 bits share
+int check_mx4(const dg4_layer_cfg* cfg, const void* S, int64_t row_begin, int64_t row_end)
+{
+    const int rc = check_cfg(cfg, false);
+    if (rc != DG4_OK) return rc;
+    return !S || !aligned16(S) || row_begin < 0 || row_end < row_begin ? (int)DG4_EINVAL : (int)DG4_OK;
+}
+bool packed_mx4(const void* packed, int64_t bytes, int k, int n)
+{
+    return packed && !((uintptr_t)packed & 255) && bytes >= dg4_mx4_bytes(k, n);
 }
 
 }  // namespace
@@ -440,21 +480,143 @@ extern "C" int dg4_sparse_attn_kv8_fwd(const dg4_layer_cfg* cfg, int32_t format,
     if (!g) return DG4_EINVAL;
     int rc = check_kv8(cfg, format, ids, codes, scales, g->n, row_begin, row_end);
     if (rc != DG4_OK) return rc;
-    if (!Q || !rel_bias || !A || !aligned16(Q, A) || ((uintptr_t)rel_bias & 3) || g->hops != cfg->hops) return DG4_EINVAL;
-    if (row_end == row_begin || g->n == 0) return DG4_OK;
-    if (A != Q && overlap(cfg, A, Q, row_end - row_begin)) return DG4_EINVAL;
-    rc = dg4_graph_ensure_device(g);
-    if (rc != DG4_OK) return rc;
-    int dev = -1;
-    if (hipGetDevice(&dev) != hipSuccess) return DG4_EHIP;
-    if (dev != g->device) return DG4_EINVAL;
     dg4_kv8_attn_args a{};
-    a.q = Q; a.a = A;
-    a.codes = codes; a.scales = scales; a.n = g->n;
-    a.rel_bias = rel_bias;
-    a.ell = g->d_ell_id; a.ell_w = g->ell_w;
-    a.ids = ids; a.row_begin = row_begin; a.row_end = row_end;
+    bool todo;
+    rc = attn_over_store(cfg, g, row_begin, row_end, ids, Q, codes, scales, rel_bias, A, &a, &todo);
+    if (rc != DG4_OK || !todo) return rc;
     HIPCHK(dg4_launch_kv8_attn(cfg->dtype, format, cfg->hidden, a, (hipStream_t)stream));
+    return DG4_OK;
+}
+
+extern "C" int dg4_kv4_write(const dg4_layer_cfg* cfg, const void* K, const void* V,
+                             int64_t row_begin, int64_t row_end, const int32_t* ids,
+                             uint8_t* codes, uint8_t* scales, int64_t n_store, void* stream)
+{
+    const int rc = check_store(cfg, ids, codes, scales, n_store, row_begin, row_end);
+    if (rc != DG4_OK) return rc;
+    if (!K || !V || !aligned16(K, V)) return DG4_EINVAL;
+    if (row_end == row_begin || n_store == 0) return DG4_OK;
+    dg4_kv8_args a{};
+    a.k = K; a.v = V;
+    a.codes = codes; a.scales = scales; a.n_store = n_store;
+    a.ids = ids; a.row_begin = row_begin; a.row_end = row_end;
+    HIPCHK(dg4_launch_kv4_write(cfg->dtype, cfg->hidden, a, (hipStream_t)stream));
+    return DG4_OK;
+}
+
+extern "C" int dg4_kv4_read(const dg4_layer_cfg* cfg, const uint8_t* codes, const uint8_t* scales,
+                            int64_t n_store, const int32_t* ids, int64_t row_begin, int64_t row_end,
+                            void* K, void* V, void* stream)
+{
+    const int rc = check_store(cfg, ids, codes, scales, n_store, row_begin, row_end);
+    if (rc != DG4_OK) return rc;
+    if (!K || !V || !aligned16(K, V)) return DG4_EINVAL;
+    if (row_end == row_begin || n_store == 0) return DG4_OK;
+    if (overlap(cfg, K, V, row_end - row_begin)) return DG4_EINVAL;
+    dg4_kv8_args a{};
+    a.k_out = K; a.v_out = V;
+    a.codes = const_cast<uint8_t*>(codes); a.scales = const_cast<uint8_t*>(scales); a.n_store = n_store;
+    a.ids = ids; a.row_begin = row_begin; a.row_end = row_end;
+    HIPCHK(dg4_launch_kv4_read(cfg->dtype, cfg->hidden, a, (hipStream_t)stream));
+    return DG4_OK;
+}
+
+extern "C" int dg4_sparse_attn_kv4_fwd(const dg4_layer_cfg* cfg, dg4_graph* g,
+                                       int64_t row_begin, int64_t row_end, const int32_t* ids,
+                                       const void* Q, const uint8_t* codes, const uint8_t* scales,
+                                       const float* rel_bias, void* A, void* stream)
+{
+    if (!g) return DG4_EINVAL;
+    int rc = check_store(cfg, ids, codes, scales, g->n, row_begin, row_end);
+    if (rc != DG4_OK) return rc;
+    dg4_kv8_attn_args a{};
+    bool todo;
+    rc = attn_over_store(cfg, g, row_begin, row_end, ids, Q, codes, scales, rel_bias, A, &a, &todo);
+    if (rc != DG4_OK || !todo) return rc;
+    HIPCHK(dg4_launch_kv4_attn(cfg->dtype, cfg->hidden, a, (hipStream_t)stream));
+    return DG4_OK;
+}
+
+extern "C" int64_t dg4_mx4_packed_bytes(const dg4_layer_cfg* cfg, int32_t k, int32_t n)
+{
+    const int rc = check_cfg(cfg, false);
+    if (rc != DG4_OK) return rc;
+    const int d = cfg->hidden;
+    if (!(k == d && (n == 3 * d || n == 4 * d)) && !(k == 4 * d && n == d)) return DG4_EUNSUPPORTED;
+    return dg4_mx4_bytes(k, n);
+}
+
+extern "C" int dg4_mx4_pack(const dg4_layer_cfg* cfg, const void* W, int32_t k, int32_t n,
+                            void* packed, int64_t packed_bytes, void* stream)
+{
+    const int64_t need = dg4_mx4_packed_bytes(cfg, k, n);
+    if (need < 0) return (int)need;
+    if (!W || !aligned16(W)) return DG4_EINVAL;
+    if (!packed_mx4(packed, packed_bytes, k, n)) return DG4_EWORKSPACE;
+    dg4_mx4_pack_args a{};
+    a.w = W; a.k = k; a.n = n;
+    a.packed = packed;
+    HIPCHK(dg4_launch_mx4_pack(cfg->dtype, a, (hipStream_t)stream));
+    return DG4_OK;
+}
+
+extern "C" int dg4_qkv_proj_mx4(const dg4_layer_cfg* cfg, const void* packed, int64_t packed_bytes,
+                                const void* S, int64_t row_begin, int64_t row_end, void* Q, void* K, void* V, void* stream)
+{
+    const int rc = check_mx4(cfg, S, row_begin, row_end);
+    if (rc != DG4_OK) return rc;
+    if (!Q || !K || !V || !aligned16(Q, K, V)) return DG4_EINVAL;
+    if (!packed_mx4(packed, packed_bytes, cfg->hidden, 3 * cfg->hidden)) return DG4_EWORKSPACE;
+    const int64_t rows = row_end - row_begin;
+    if (rows == 0) return DG4_OK;
+    for (const void* out : { Q, K, V }) if (overlap(cfg, S, out, rows)) return DG4_EINVAL;
+    if (overlap(cfg, Q, K, rows) || overlap(cfg, Q, V, rows) || overlap(cfg, K, V, rows)) return DG4_EINVAL;
+    dg4_mx4_proj_args a{};
+    a.s = S; a.w_packed = packed;
+    a.out[0] = Q; a.out[1] = K; a.out[2] = V;
+    a.row_begin = row_begin; a.row_end = row_end;
+    HIPCHK(dg4_launch_mx4_proj(cfg->dtype, cfg->hidden, a, (hipStream_t)stream));
+    return DG4_OK;
+}
+
+extern "C" int dg4_qkv_proj_kv4(const dg4_layer_cfg* cfg, const void* packed, int64_t packed_bytes,
+                                const void* S, int64_t row_begin, int64_t row_end, const int32_t* ids,
+                                void* Q, uint8_t* codes, uint8_t* scales, int64_t n_store, void* stream)
+{
+    const int rc = check_store(cfg, ids, codes, scales, n_store, row_begin, row_end);
+    if (rc != DG4_OK) return rc;
+    if (!S || !Q || !aligned16(S, Q)) return DG4_EINVAL;
+    if (!packed_mx4(packed, packed_bytes, cfg->hidden, 3 * cfg->hidden)) return DG4_EWORKSPACE;
+    const int64_t rows = row_end - row_begin;
+    if (rows == 0) return DG4_OK;
+    if (overlap(cfg, S, Q, rows)) return DG4_EINVAL;
+    dg4_mx4_proj_args a{};
+    a.s = S; a.w_packed = packed;
+    a.out[0] = Q;
+    a.codes = codes; a.scales = scales; a.n_store = n_store;
+    a.ids = ids; a.row_begin = row_begin; a.row_end = row_end;
+    HIPCHK(dg4_launch_mx4_proj(cfg->dtype, cfg->hidden, a, (hipStream_t)stream));
+    return DG4_OK;
+}
+
+extern "C" int dg4_ffn_mx4_fwd(const dg4_layer_cfg* cfg, const void* packed_W1, int64_t packed_W1_bytes,
+                               const void* packed_W2, int64_t packed_W2_bytes,
+                               const void* S, int64_t row_begin, int64_t row_end, void* Out, void* stream)
+{
+    const int rc = check_mx4(cfg, S, row_begin, row_end);
+    if (rc != DG4_OK) return rc;
+    if (!Out || !aligned16(Out)) return DG4_EINVAL;
+    const int d = cfg->hidden;
+    if (!packed_mx4(packed_W1, packed_W1_bytes, d, 4 * d) || !packed_mx4(packed_W2, packed_W2_bytes, 4 * d, d)) return DG4_EWORKSPACE;
+    const int64_t rows = row_end - row_begin;
+    if (rows == 0) return DG4_OK;
+    if (overlap(cfg, S, Out, rows)) return DG4_EINVAL;
+    dg4_mx4_ffn_args a{};
+    a.s = S; a.out = Out;
+    a.w1_packed = packed_W1; a.w2_packed = packed_W2;
+    a.row_begin = row_begin; a.row_end = row_end;
+    a.ln_eps = cfg->ln_eps;
+    HIPCHK(dg4_launch_mx4_ffn(cfg->dtype, d, a, (hipStream_t)stream));
     return DG4_OK;
 }
 

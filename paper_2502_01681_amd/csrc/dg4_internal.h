@@ -12,6 +12,7 @@
 
 #include "dg4.h"
 #include "dg4_serving.h"
+#include "dg4_mx4.h"
 
 // Neighbour rows on the device: fixed-width rows of packed 32-bit entries
 // (relation code << 30 | index), padded with DG4_ELL_PAD. Width = 2^(hops+1), at least 8:
@@ -348,11 +349,11 @@ struct dg4_bulk_args {
 int dg4_launch_pack_w32(const void* w, int ld, void* packed, hipStream_t s);   // [256, 768] weights, row stride ld
 int dg4_launch_bulk_proj(const dg4_bulk_args& a, hipStream_t s);
 
-// ---- the K|V store in 8 bits (dg4_kv8.hip) ----
+// ---- the K|V stores in 8 bits (dg4_kv8.hip) and in 4 (dg4_kv4.hip) ----
 struct dg4_kv8_args {
     const void* k; const void* v;          // write: [*, d] rows
     void* k_out; void* v_out;              // read: [*, d] rows
-    uint8_t* codes;                        // [n_store, 2d] K | V
+    uint8_t* codes;                        // [n_store, 2d] K | V; in 4 bits [n_store, d], two codes to a byte
     uint8_t* scales;                       // [n_store, heads, 2] biased exponents of K and V
     const int32_t* ids;                    // nullable: store row of row r is ids[r], else r; none if outside [0, n_store)
     int64_t n_store;
@@ -369,6 +370,36 @@ struct dg4_kv8_attn_args {
 int dg4_launch_kv8_write(int dtype, int format, int hidden, const dg4_kv8_args& a, hipStream_t s);
 int dg4_launch_kv8_read(int dtype, int format, int hidden, const dg4_kv8_args& a, hipStream_t s);
 int dg4_launch_kv8_attn(int dtype, int format, int hidden, const dg4_kv8_attn_args& a, hipStream_t s);
+int dg4_launch_kv4_write(int dtype, int hidden, const dg4_kv8_args& a, hipStream_t s);
+int dg4_launch_kv4_read(int dtype, int hidden, const dg4_kv8_args& a, hipStream_t s);
+int dg4_launch_kv4_attn(int dtype, int hidden, const dg4_kv8_attn_args& a, hipStream_t s);
+
+// ---- products of rows and weights in 4 bits (dg4_mx4.hip) ----
+struct dg4_mx4_pack_args {
+    const void* w;                         // [k, n]
+    int k, n;                              // multiples of 64 and 32
+    void* packed;                          // dg4_mx4_bytes(k, n)
+};
+struct dg4_mx4_proj_args {
+    const void* s;                         // [*, d] rows
+    const void* w_packed;                  // of [d, 3d]
+    void* out[3];                          // Q, K, V [*, d] rows; into a store, Q alone
+    uint8_t* codes;                        // nullable: [n_store, d] K | V, two codes to a byte
+    uint8_t* scales;                       // [n_store, heads, 2]
+    const int32_t* ids;                    // nullable: store row of row r is ids[r], else r; none if outside [0, n_store)
+    int64_t n_store;
+    int64_t row_begin, row_end;
+};
+struct dg4_mx4_ffn_args {
+    const void* s; void* out;              // [*, d] rows
+    const void* w1_packed; const void* w2_packed;              // of [d, 4d] and [4d, d]
+    int64_t row_begin, row_end;
+    float ln_eps;
+};
+int64_t dg4_mx4_bytes(int k, int n);
+int dg4_launch_mx4_pack(int dtype, const dg4_mx4_pack_args& a, hipStream_t s);
+int dg4_launch_mx4_proj(int dtype, int hidden, const dg4_mx4_proj_args& a, hipStream_t s);
+int dg4_launch_mx4_ffn(int dtype, int hidden, const dg4_mx4_ffn_args& a, hipStream_t s);
 
 // ---- Q|K|V projection with low-rank adapters (dg4_lora.hip) ----
 struct dg4_lora_pack_args {
@@ -405,6 +436,9 @@ DG4_CHECK_KERNEL_ARGS(dg4_bulk_args);
 DG4_CHECK_KERNEL_ARGS(dg4_heads_args);
 DG4_CHECK_KERNEL_ARGS(dg4_kv8_args);
 DG4_CHECK_KERNEL_ARGS(dg4_kv8_attn_args);
+DG4_CHECK_KERNEL_ARGS(dg4_mx4_pack_args);
+DG4_CHECK_KERNEL_ARGS(dg4_mx4_proj_args);
+DG4_CHECK_KERNEL_ARGS(dg4_mx4_ffn_args);
 DG4_CHECK_KERNEL_ARGS(dg4_lora_pack_args);
 DG4_CHECK_KERNEL_ARGS(dg4_lora_args);
 DG4_CHECK_KERNEL_ARGS(dg4_heads_pack_args);
