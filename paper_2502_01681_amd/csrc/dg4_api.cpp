@@ -210,6 +210,7 @@ int attn_over_store(const dg4_layer_cfg* cfg, dg4_graph* g, int64_t row_begin, i
     a->codes = codes; a->scales = scales; a->n = g->n;
     a->rel_bias = rel_bias;
     a->ell = g->d_ell_id; a->ell_w = g->ell_w;
+    a->most = (2 << g->hops) - 1;
     a->ids = ids; a->row_begin = row_begin; a->row_end = row_end;
     *todo = true;
     return DG4_OK;

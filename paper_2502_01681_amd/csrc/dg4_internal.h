@@ -364,6 +364,7 @@ struct dg4_kv8_attn_args {
     const uint8_t* codes; const uint8_t* scales; int64_t n;
     const float* rel_bias;                 // [heads, 4]
     const uint32_t* ell; int ell_w;        // neighbour rows by node id
+    int most;                              // entries that a row can have
     const int32_t* ids;                    // nullable: the gate of row r is ids[r], else r; none if outside [0, n)
     int64_t row_begin, row_end;
 };

@@ -24,7 +24,7 @@ constexpr uint32_t KV4_NEAR_BYTES = 0xC0000000u;
 // runs of 128 workgroups go to one XCD, so that its L2 serves them. What is left behind the last eight whole runs goes in turn.
 __device__ __forceinline__ uint32_t kv4_block(uint32_t block, uint32_t blocks)
 {
-    constexpr uint32_t RUN = 128;
+    constexpr uint32_t RUN = 64;
     const uint32_t base = block / (8 * RUN) * (8 * RUN);
     return base + 8 * RUN <= blocks ? base + block % 8 * RUN + (block - base) / 8 : block;
 }
@@ -41,7 +41,7 @@ __global__ __launch_bounds__(256) void kv4_write_kernel(dg4_kv8_args p)
     const bool is_v = sub >= LPG / 2;
     const int col = (sub % (LPG / 2)) * 8;
     const T* src = (const T*)(is_v ? p.v : p.k) + col;
-    Eighth<T> x[U];
+    Values<T, 8> x[U];
     int64_t at[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -54,10 +54,12 @@ __global__ __launch_bounds__(256) void kv4_write_kernel(dg4_kv8_args p)
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const uint32_t byte = fp4_scale_byte(max_of_4_lanes(x[u].top()));
-        const uint32_t w = byte == FP4_BAD ? 0u : x[u].codes(byte);
+        const uint32_t byte = fp4_scale_byte(max_of_lanes<4>(x[u].top()));
+        uint32_t w[1];
+        x[u].codes(byte << 23, w);
+        if (byte == FP4_BAD) w[0] = 0;
         if (at[u] >= 0) {
-            *(uint32_t*)(p.codes + at[u] * D + sub * 4) = w;
+            *(uint32_t*)(p.codes + at[u] * D + sub * 4) = w[0];
             if ((sub & 3) == 0) p.scales[at[u] * (2 * D / 32) + col / 32 * 2 + (is_v ? 1 : 0)] = (uint8_t)byte;
         }
     }
@@ -209,9 +211,10 @@ template <> struct HeadQ<bf16_t> {
 template <typename T, int D, int S, int CH, bool ONCE, bool FAR>
 __global__ __launch_bounds__(256) void kv4_attn_kernel(dg4_kv8_attn_args p)
 {
-    constexpr int LPR = D / 32, HEADS = D / 32, GPW = 64 / LPR;
+    constexpr int LPR = D / 32, HEADS = D / 32, GPW = 64 / LPR, QUADS = (CH + 3) / 4;
     constexpr int RPW = GPW / S;                  // rows per wave
     constexpr uint32_t NONE = KV4_NEAR_BYTES / D; // past the end of a store that buffer addressing reaches
+    static_assert(S == 1 && ONCE || CH % 4 == 0, "a group's entries are whole pieces of 16 bytes");
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int head = lane % LPR, group = lane / LPR, part = group % S;
     // biases of a head by relation code
@@ -219,26 +222,30 @@ __global__ __launch_bounds__(256) void kv4_attn_kernel(dg4_kv8_attn_args p)
     if (threadIdx.x < HEADS * 4) bias[threadIdx.x / 4][threadIdx.x % 4] = p.rel_bias[threadIdx.x];
     __syncthreads();
     const int64_t r = p.row_begin + ((int64_t)(ONCE ? kv4_block(blockIdx.x, gridDim.x) : blockIdx.x) * 4 + wave) * RPW + group / S;
-    // (what leaves here leaves as whole rows)
-    if (r >= p.row_end) return;
-    const int64_t v = p.ids ? (int64_t)p.ids[r] : r;
-    if (v < 0 || v >= p.n) return;
+    // (a row that is none goes along with the first gate's, if its wave holds another, and is not written)
+    int64_t v = -1;
+    if (r < p.row_end) v = p.ids ? (int64_t)p.ids[r] : r;
+    const bool in = v >= 0 && v < p.n;
+    const uint64_t rows_in = __ballot(in);
+    if (rows_in == 0) return;
+    if (!in) v = 0;
 
     const dg4_i32x4 code_bytes = row_buffer(p.codes, 0, FAR ? 0 : (uint32_t)(p.n * D));
     const dg4_i32x4 scale_bytes = row_buffer(p.scales, 0, FAR ? 0 : (uint32_t)(p.n * 2 * HEADS));
     const uint32_t* erow = p.ell + v * (int64_t)p.ell_w;
-    uint4 ent[CH / 4];
+    uint4 ent[QUADS];
     auto entries = [&](int c0) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < CH / 4; ++i)
+        for (int i = 0; i < QUADS; ++i)
             ent[i] = c0 + 4 * i < p.ell_w ? *(const uint4*)(erow + c0 + 4 * i) : make_uint4(DG4_ELL_PAD, DG4_ELL_PAD, DG4_ELL_PAD, DG4_ELL_PAD);
     };
     entries(part * CH);
     HeadQ<T> q;
-    q.load((const T*)p.q + r * D + head * 32);
-    // the same for all lanes of the row, so that a row does not see its neighbours
+    q.load((const T*)p.q + (in ? r : p.row_begin) * D + head * 32);
+    // whether it is so for some lane of the row: a row does not see its neighbours
     constexpr int LANES = LPR * S;
-    const bool odd = (__ballot(q.odd()) >> (lane / LANES * LANES) & (~0ull >> (64 - LANES))) != 0;
+    auto some = [&](bool x) __attribute__((always_inline)) { return (__ballot(x) >> (lane / LANES * LANES) & (~0ull >> (64 - LANES))) != 0; };
+    const bool odd = some(q.odd());
     const float c = 0.17677669529663687f;         // 1/sqrt(32)
     const float log2e = 1.4426950408889634f;      // (not taken into the scores: the lowest bias times this is no number)
     float m = -INFINITY, z = 0.f;
@@ -294,27 +301,30 @@ __global__ __launch_bounds__(256) void kv4_attn_kernel(dg4_kv8_attn_args p)
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
-        // (Nothing so far, -inf: any finite base will do, every weight is 0.)
-        const float base = cm == -INFINITY ? 0.f : cm;
-        if constexpr (!ONCE) {
-            const float corr = __builtin_amdgcn_exp2f((m - base) * log2e);
+        // What weights are relative to: the maximum; where there are steps to come, what it was when some lane of the row's last was more than 4
+        // past it, so that few steps have sums to scale down. e^4 < 2^6, which every weight there is divided by: no sum of V is larger than it
+        // would be, and a source alone in its row still leaves as it is. (Nothing so far, -inf: any finite base will do, every weight is 0.)
+        if constexpr (ONCE) {
+            m = cm;
+        } else if (some(cm > m + 4.f)) {
+            const float corr = __builtin_amdgcn_exp2f((m - (cm == -INFINITY ? 0.f : cm)) * log2e);
+            m = cm;
             z *= corr;
 #pragma unroll
             for (int i = 0; i < 32; ++i) acc[i] *= corr;
         }
-        m = cm;
+        const float base = m == -INFINITY ? 0.f : m;
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
-            const float pj = __builtin_amdgcn_exp2f((s[j] - base) * log2e);
+            const float pj = __builtin_amdgcn_exp2f(ONCE ? (s[j] - base) * log2e : fmaf(s[j] - base, log2e, -6.f));
             z += pj;
-            const float pv = pj * fp4_scale_value(sw[j] >> 8);
             const uint32_t words[4] = { vw[j].x, vw[j].y, vw[j].z, vw[j].w };
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 float x[8];
-                fp4_get8(words[i], 127, x);
+                fp4_get8(words[i], sw[j] >> 8, x);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) acc[8 * i + k] = ONCE && j == 0 ? pv * x[k] : fmaf(pv, x[k], acc[8 * i + k]);
+                for (int k = 0; k < 8; ++k) acc[8 * i + k] = ONCE && j == 0 ? pj * x[k] : fmaf(pj, x[k], acc[8 * i + k]);
             }
         }
         if constexpr (ONCE) break;
@@ -341,14 +351,13 @@ __global__ __launch_bounds__(256) void kv4_attn_kernel(dg4_kv8_attn_args p)
             }
             first += upper ? half : 0;
         };
-        static_assert(S <= 16 && KEPT % 2 == 0, "exchanges");
+        static_assert(S <= 16, "exchanges");
         if constexpr (S >= 16) halve(std::integral_constant<int, 8>{});
         if constexpr (S >= 8) halve(std::integral_constant<int, 4>{});
         if constexpr (S >= 4) halve(std::integral_constant<int, 2>{});
         halve(std::integral_constant<int, 1>{});
     }
     const float rz = z == 0.f ? 0.f : 1.0f / z;
-    T* out = (T*)p.a + r * D + head * 32 + first;
     constexpr int WORDS = KEPT * (int)sizeof(T) / 4;
     uint32_t w[WORDS];
 #pragma unroll
@@ -356,13 +365,26 @@ __global__ __launch_bounds__(256) void kv4_attn_kernel(dg4_kv8_attn_args p)
         if constexpr (sizeof(T) == 2) w[i / 2] = pack_bf16x2(acc[i] * rz, acc[i + 1] * rz);
         else { w[i] = __float_as_uint(acc[i] * rz); w[i + 1] = __float_as_uint(acc[i + 1] * rz); }
     }
-    if constexpr (WORDS >= 4) {
+    if constexpr (WORDS > 4) {
+        // A lane's pieces of 16 bytes go through LDS (the wave's own part of it), so that a store is whole rows: 64 pieces side by side
+        constexpr int PIECES = WORDS / 4, PPR = D * (int)sizeof(T) / 16;
+        __shared__ uint4 stage[4][64 * (PIECES + 1)];
+        const int place = ((group / S) * LPR + head) * S + first / KEPT;
 #pragma unroll
-        for (int i = 0; i < WORDS; i += 4) store_stream(out + i * (4 / (int)sizeof(T)), make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]));
-    } else if constexpr (WORDS == 2) {
-        *(uint2*)out = make_uint2(w[0], w[1]);
-    } else {
-        *(uint32_t*)out = w[0];
+        for (int i = 0; i < PIECES; ++i) stage[wave][place * (PIECES + 1) + i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        const int64_t r0 = r - group / S;         // the wave's first row
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const int piece = lane + 64 * i;
+            const uint4 x = stage[wave][piece / PIECES * (PIECES + 1) + piece % PIECES];
+            if (rows_in >> (piece / PPR * LANES) & 1) store_stream((T*)p.a + r0 * D + piece * (16 / (int)sizeof(T)), x);
+        }
+    } else if (in) {
+        T* out = (T*)p.a + r * D + head * 32 + first;
+        if constexpr (WORDS == 4) store_stream(out, make_uint4(w[0], w[1], w[2], w[3]));
+        else if constexpr (WORDS == 2) *(uint2*)out = make_uint2(w[0], w[1]);
+        else *(uint32_t*)out = w[0];
     }
 }
 
@@ -393,17 +415,26 @@ int launch_read(const dg4_kv8_args& args, hipStream_t s)
         hipLaunchKernelGGL((kv4_read_kernel<T, D, U>), grid, dim3(256), 0, s, a);
     });
 }
-// The split goes by the table's width alone, so a row's result does not depend on which rows a call covers.
-template <typename T, int D, bool FAR>
-int launch_attn_from(const dg4_kv8_attn_args& args, hipStream_t s)
+// The split of a row goes by the cones' depth alone, so its result does not depend on which rows a call covers. A cone of one hop
+// holds three gates, of two hops seven, fifteen, ...; MOST: what a call's cones hold at most.
+template <typename T, int D, bool FAR, int MOST>
+int launch_attn_of(const dg4_kv8_attn_args& args, hipStream_t s)
 {
     constexpr int GPW = 64 / (D / 32);
-    const bool once = args.ell_w <= 16;
-    return launch_rows(args, once ? 4 * GPW / 2 : 4 * GPW / 8, [&](const dg4_kv8_attn_args& a, dim3 grid) {
-        if (a.ell_w <= 8) hipLaunchKernelGGL((kv4_attn_kernel<T, D, 2, 4, true, FAR>), grid, dim3(256), 0, s, a);
-        else if (once) hipLaunchKernelGGL((kv4_attn_kernel<T, D, 2, 8, true, FAR>), grid, dim3(256), 0, s, a);
-        else hipLaunchKernelGGL((kv4_attn_kernel<T, D, 8, 4, false, FAR>), grid, dim3(256), 0, s, a);
+    constexpr bool ONCE = MOST <= 15;
+    constexpr int S = MOST <= 7 ? 1 : MOST <= 31 ? 2 : MOST <= 127 ? 4 : MOST <= 255 ? 8 : GPW;
+    constexpr int CH = MOST <= 7 ? MOST : ONCE ? 8 : 4;
+    return launch_rows(args, 4 * GPW / S, [&](const dg4_kv8_attn_args& a, dim3 grid) {
+        hipLaunchKernelGGL((kv4_attn_kernel<T, D, S, CH, ONCE, FAR>), grid, dim3(256), 0, s, a);
     });
+}
+template <typename T, int D, bool FAR>
+int launch_attn_from(const dg4_kv8_attn_args& a, hipStream_t s)
+{
+    return a.most <= 3 ? launch_attn_of<T, D, FAR, 3>(a, s) : a.most <= 7 ? launch_attn_of<T, D, FAR, 7>(a, s)
+         : a.most <= 15 ? launch_attn_of<T, D, FAR, 15>(a, s) : a.most <= 31 ? launch_attn_of<T, D, FAR, 31>(a, s)
+         : a.most <= 127 ? launch_attn_of<T, D, FAR, 127>(a, s) : a.most <= 255 ? launch_attn_of<T, D, FAR, 255>(a, s)
+         : launch_attn_of<T, D, FAR, 511>(a, s);
 }
 template <typename T, int D>
 int launch_attn(const dg4_kv8_attn_args& a, hipStream_t s)

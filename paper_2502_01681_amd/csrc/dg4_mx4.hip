@@ -46,7 +46,8 @@ __global__ __launch_bounds__(256) void mx4_pack_kernel(dg4_mx4_pack_args p)
     }
     const uint32_t byte = fp4_scale_byte(top);
     uint4 w = make_uint4(0, 0, 0, 0);
-    if (byte != FP4_BAD) w = make_uint4(fp4_put8(x, byte), fp4_put8(x + 8, byte), fp4_put8(x + 16, byte), fp4_put8(x + 24, byte));
+    const uint32_t scale = byte << 23;
+    if (byte != FP4_BAD) w = make_uint4(fp4_put8(x, scale), fp4_put8(x + 8, scale), fp4_put8(x + 16, scale), fp4_put8(x + 24, scale));
     // column 16 hi + 4 a + b is operand row 8 a + 4 hi + b
     const int in_tile = col % 32, tile = col / 32, m = 8 * ((in_tile >> 2) & 3) + 4 * (in_tile >> 4) + (in_tile & 3);
     const int c = block / 2, lane = block % 2 * 32 + m;
@@ -71,57 +72,109 @@ template <int N, int C = 0, typename F> __device__ __forceinline__ void each(F&&
     }
 }
 
-// Rows in 4 bits in LDS, as B operand: 16 bytes of codes per block, a word of scale bytes for every eight blocks of one parity
+// Rows in 4 bits in LDS, as B operand: 16 bytes of codes per block, a word of scale bytes for every four chunks and parity of the block
 template <int D> struct MxRows {
     static constexpr int STRIDE = D / 2 + 16;     // bytes
     static constexpr int WORDS = (D / 32 + 7) / 8 * 2;         // scale words of a row
     uint8_t codes[ROWS][STRIDE];
-    uint32_t scales[ROWS][WORDS];
+    uint32_t scales[WORDS][ROWS];
     __device__ __forceinline__ uint8_t* scale_at(int row, int block)
     {
-        return (uint8_t*)&scales[row][block / 8 * 2 + block % 2] + block / 2 % 4;
+        return (uint8_t*)&scales[block / 8 * 2 + block % 2][row] + block / 2 % 4;
     }
+    __device__ __forceinline__ uint4 operand(int n, int hi, int c) const { return *(const uint4*)(codes[n] + (2 * c + hi) * 16); }
+    __device__ __forceinline__ uint32_t scale(int n, int hi, int c) const { return scales[c / 4 * 2 + hi][n]; }
 };
 
-// A tile's rows of S: a thread takes pieces of eight features, PIECES of them, 2 D threads to a workgroup
-template <typename T, int D> struct TileRows {
-    static constexpr int PPR = D / 8, PIECES = ROWS * PPR / (2 * D);
-    Eighth<T> x[PIECES];
-    __device__ __forceinline__ void load(const T* s, int64_t r0, int64_t r_end)
+// Rows as they are, in LDS
+template <typename T, int D> struct FullRows { T x[ROWS][D + 16 / (int)sizeof(T)]; };
+
+// Rows of a tile as a buffer: what lies behind the call's last row reads as zeros and is not written, without a branch (behind
+// which a wait for loads would be one for every store before it, too). No rows at all (r0 past the end, or not yet there): nothing.
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+__device__ i32x4 dg4_raw_buffer_load16(i32x4 rsrc, int voffset, int soffset, int aux) __asm("llvm.amdgcn.raw.buffer.load.v4i32");
+__device__ void dg4_raw_buffer_store16(i32x4 v, i32x4 rsrc, int voffset, int soffset, int aux) __asm("llvm.amdgcn.raw.buffer.store.v4i32");
+template <typename T, int D> __device__ __forceinline__ i32x4 tile_buffer(const void* rows, int64_t r0, int64_t r_end)
+{
+    const uint64_t a = (uint64_t)rows + (uint64_t)r0 * (D * sizeof(T));
+    const int n = (int)max((int64_t)0, min((int64_t)ROWS, r_end - r0));
+    return i32x4{ (int)(uint32_t)a, (int)((uint32_t)(a >> 32) & 0xFFFFu), n * (D * (int)sizeof(T)), 0x00020000 };
+}
+
+// A tile's rows of S, in pieces of half a block to each of THREADS threads
+template <typename T, int D, int THREADS> struct TileRows {
+    static constexpr int PPR = D / 16, PIECES = ROWS * PPR / THREADS;
+    static_assert(PIECES * THREADS == ROWS * PPR, "whole pieces");
+    Values<T, 16> x[PIECES];
+    __device__ __forceinline__ void load(const void* s, int64_t r0, int64_t r_end)
     {
+        const i32x4 tile = tile_buffer<T, D>(s, r0, r_end);
 #pragma unroll
-        for (int i = 0; i < PIECES; ++i) {
-            const int piece = (int)threadIdx.x + 2 * D * i;
-            x[i].load(s + min(r0 + piece / PPR, r_end - 1) * D + piece % PPR * 8);
-        }
+        for (int k = 0; k < PIECES; ++k)
+#pragma unroll
+            for (int i = 0; i < Values<T, 16>::PIECES; ++i)
+                x[k].w[i] = __builtin_bit_cast(uint4, dg4_raw_buffer_load16(tile, ((int)threadIdx.x + k * THREADS) * (16 * (int)sizeof(T)) + 16 * i, 0, 0));
     }
     __device__ __forceinline__ void put(MxRows<D>& to) const
     {
 #pragma unroll
-        for (int i = 0; i < PIECES; ++i) {
-            const int piece = (int)threadIdx.x + 2 * D * i, row = piece / PPR, sub = piece % PPR;
-            const uint32_t byte = fp4_scale_byte(max_of_4_lanes(x[i].top()));
-            *(uint32_t*)(to.codes[row] + sub * 4) = byte == FP4_BAD ? 0u : x[i].codes(byte);
-            if (sub % 4 == 0) *to.scale_at(row, sub / 4) = (uint8_t)byte;
+        for (int k = 0; k < PIECES; ++k) {
+            const int piece = (int)threadIdx.x + k * THREADS, row = piece / PPR, sub = piece % PPR;
+            const uint32_t top = max_of_lanes<2>(x[k].top()), scale = fp4_scale_bits(top);
+            const uint32_t byte = top >= 0x7F800000u ? FP4_BAD : scale >> 23;
+            uint32_t c[2];
+            x[k].codes(scale, c);                 // (any, where the byte says that they are none)
+            *(uint2*)(to.codes[row] + sub * 8) = make_uint2(c[0], c[1]);
+            *to.scale_at(row, sub / 2) = (uint8_t)byte;        // (the block's other lane the same)
+        }
+    }
+    __device__ __forceinline__ void keep(FullRows<T, D>& to) const
+    {
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) {
+            const int piece = (int)threadIdx.x + k * THREADS;
+            x[k].store(to.x[piece / PPR] + piece % PPR * 16);
         }
     }
 };
 
-// Half a block, a lane's sixteen accumulators, in 4 bits; the other half is lane ^ 32's. (A NaN, which an ordinary maximum passes
-// over, makes the block one that is not finite.)
-__device__ __forceinline__ uint2 half_block(const float* x, uint32_t& byte)
+// A lane's value and that of lane ^ 32
+struct Pair { float a, b; };
+__device__ __forceinline__ Pair both_halves(float x)
 {
-    uint32_t top = 0;
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return { __uint_as_float(r[0]), __uint_as_float(r[1]) };
+}
+// The largest magnitude, as bits, of a block of which a lane has sixteen values and lane ^ 32 the others. LOWER: what is below zero counts
+// as zero. (The maximum keeps a NaN, whose bits are above infinity's whatever its sign.)
+template <bool LOWER> __device__ __forceinline__ uint32_t block_top(const f32x16& x)
+{
+    float top = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
-    top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-    byte = fp4_scale_byte(top);
-    return byte == FP4_BAD ? make_uint2(0, 0) : make_uint2(fp4_put8(x, byte), fp4_put8(x + 8, byte));
+    for (int i = 0; i < 16; ++i) top = __builtin_elementwise_maximum(top, LOWER ? x[i] : fabsf(x[i]));
+    const Pair p = both_halves(top);
+    return __float_as_uint(__builtin_elementwise_maximum(p.a, p.b));
+}
+__device__ __forceinline__ uint2 half_codes(const f32x16& x, uint32_t scale_bits)
+{
+    float v[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = x[i];
+    return make_uint2(fp4_put8(v, scale_bits), fp4_put8(v + 8, scale_bits));
+}
+// Codes below zero to (minus) zero
+__device__ __forceinline__ uint32_t no_less_than_zero(uint32_t w)
+{
+    const uint32_t t = w & 0x88888888u;
+    return w & ~(t - (t >> 3));
 }
 
 // Sixteen neighbouring values of a row
-template <typename T> __device__ __forceinline__ void put16(T* to, const float* x)
+template <typename T> __device__ __forceinline__ void put16(T* to, const f32x16& v)
 {
+    float x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = v[i];
     if constexpr (sizeof(T) == 2) {
         uint4 a, b;
         Elem<bf16_t>::pack(x, a, b);
@@ -141,6 +194,25 @@ template <typename T> __device__ __forceinline__ void get16(const T* from, float
     } else {
         Elem<float>::unpack(p[0], p[1], x);
         Elem<float>::unpack(p[2], p[3], x + 8);
+    }
+}
+
+template <typename T> __device__ __forceinline__ void put16(i32x4 tile, int at, const f32x16& v)
+{
+    float x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = v[i];
+    if constexpr (sizeof(T) == 2) {
+        uint4 a, b;
+        Elem<bf16_t>::pack(x, a, b);
+        dg4_raw_buffer_store16(__builtin_bit_cast(i32x4, a), tile, at, 0, 0);
+        dg4_raw_buffer_store16(__builtin_bit_cast(i32x4, b), tile, at + 16, 0, 0);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const i32x4 w = { (int)__float_as_uint(x[4 * i]), (int)__float_as_uint(x[4 * i + 1]), (int)__float_as_uint(x[4 * i + 2]), (int)__float_as_uint(x[4 * i + 3]) };
+            dg4_raw_buffer_store16(w, tile, at + 16 * i, 0, 0);
+        }
     }
 }
 
@@ -164,21 +236,21 @@ __global__ __launch_bounds__(2 * D) void mx4_proj_kernel(dg4_mx4_proj_args p)
         sw[j] = ((const uint32_t*)((const uint4*)p.w_packed + 3 * D / 32 * KC * 64))[tile * 64 + lane];
     }
     const int64_t step = (int64_t)gridDim.x * ROWS;
-    TileRows<T, D> x;
+    TileRows<T, D, 2 * D> x;
     int64_t r0 = p.row_begin + (int64_t)blockIdx.x * ROWS;
-    x.load((const T*)p.s, r0, p.row_end);
+    x.load(p.s, r0, p.row_end);
     for (int t = 0; r0 < p.row_end; r0 += step, t ^= 1) {
         x.put(rows[t]);
         __syncthreads();
-        if (r0 + step < p.row_end) x.load((const T*)p.s, r0 + step, p.row_end);
+        x.load(p.s, r0 + step, p.row_end);
         f32x16 acc[3];
 #pragma unroll
         for (int j = 0; j < 3; ++j)
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[j][i] = 0.f;
-        const uint32_t sb = rows[t].scales[n][hi];
+        const uint32_t sb = rows[t].scale(n, hi, 0);
         each<KC>([&](auto c) __attribute__((always_inline)) {
-            const uint4 b = *(const uint4*)(rows[t].codes[n] + (2 * c + hi) * 16);
+            const uint4 b = rows[t].operand(n, hi, c);
 #pragma unroll
             for (int j = 0; j < 3; ++j) mma_mx<c>(w[j][c], sw[j], b, sb, acc[j]);
         });
@@ -187,112 +259,197 @@ __global__ __launch_bounds__(2 * D) void mx4_proj_kernel(dg4_mx4_proj_args p)
         if (r < p.row_end) at = STORE && p.ids ? (int64_t)p.ids[r] : r;
 #pragma unroll
         for (int j = 0; j < 3; ++j) {
-            float v[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] = acc[j][i];
             if (STORE && j > 0) {
-                uint32_t byte;
-                const uint2 codes = half_block(v, byte);
+                const uint32_t byte = fp4_scale_byte(block_top<false>(acc[j]));
+                const uint2 codes = byte == FP4_BAD ? make_uint2(0, 0) : half_codes(acc[j], byte << 23);
                 if (at >= 0 && at < p.n_store) {
                     *(uint2*)(p.codes + at * D + (j - 1) * (D / 2) + wave * 16 + hi * 8) = codes;
                     if (hi == 0) p.scales[(at * HEADS + wave) * 2 + j - 1] = (uint8_t)byte;
                 }
             } else if (r < p.row_end) {
-                put16<T>((T*)p.out[j] + r * D + wave * 32 + hi * 16, v);
+                put16<T>((T*)p.out[j] + r * D + wave * 32 + hi * 16, acc[j]);
             }
         }
     }
 }
 
-// A workgroup has a wave for every 32 columns of the output and takes tiles of rows in turn. Each wave holds its share of both
-// matrices in registers: four tiles of W1's columns, and its own columns of W2. The activations of a tile go through LDS in 4 bits.
+// A workgroup of eight waves takes tiles of rows in turn; both matrices stay in its registers. Four waves, one to a SIMD, put rows into LDS and
+// form the activations, a quarter of W1's columns each; the other four multiply the activations, which go through LDS in 4 bits, by a quarter of
+// W2's columns each, and normalise. Between two barriers the former are a tile ahead of the latter: vector instructions of the one
+// (rounding to 4 bits, LayerNorm) run beside products of the other.
+// A million rows of bfloat16 at hidden 256: 326 us, 3.2 PFLOP/s, where the bytes take 199 at the rate of a copy and the products 149 at that of
+// a loop of them. A turn of a tile is 4200 cycles of each SIMD: 64 products, which keep its matrix core for 35 cycles and its vector
+// instructions from being issued for 16, and 614 vector instructions of 4 cycles, 3480 cycles in all; the clock falls to 1.8 GHz under it.
+// Eight waves that all do everything, an eighth of either matrix each, in step: 365 us (their products and vector instructions come at the same
+// time), with rows and residual from memory instead of LDS, so that waits for loads were waits for stores: 412, with three barriers to a
+// tile: 520. The same with the two halves of the waves in opposite order, or the residual added on the matrix cores: no faster.
+constexpr int FFN_THREADS = 512;
 template <typename T, int D>
-__global__ __launch_bounds__(2 * D) void mx4_ffn_kernel(dg4_mx4_ffn_args p)
+__global__ __launch_bounds__(FFN_THREADS) void mx4_ffn_kernel(dg4_mx4_ffn_args p)
 {
-    constexpr int WAVES = D / 32, KC = D / 64, KC2 = 4 * D / 64;
-    __shared__ MxRows<D> rows;
-    __shared__ MxRows<4 * D> hidden;
-    __shared__ float2 part[ROWS][WAVES];
+    constexpr int KC = D / 64, KC2 = 4 * D / 64;
+    constexpr int TILES1 = D / 32, WORDS = TILES1 / 4, TILES2 = D / 128;       // of a wave: tiles of columns, and scale words of a row that the former make up
+    __shared__ MxRows<D> rows[2];
+    __shared__ MxRows<4 * D> hidden[2];
+    __shared__ FullRows<T, D> full[3];
+    __shared__ float2 part[2][4][ROWS];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 31, hi = lane >> 5;
-    uint4 w1[4][KC], w2[KC2];
-    uint32_t sw1[4], sw2[KC2 / 4];
-    const uint4* u1 = (const uint4*)p.w1_packed;
-    const uint4* u2 = (const uint4*)p.w2_packed;
-    const uint32_t* s1 = (const uint32_t*)(u1 + 4 * D / 32 * KC * 64);
-    const uint32_t* s2 = (const uint32_t*)(u2 + D / 32 * KC2 * 64);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-#pragma unroll
-        for (int c = 0; c < KC; ++c) w1[j][c] = u1[((4 * wave + j) * KC + c) * 64 + lane];
-        sw1[j] = s1[(4 * wave + j) * 64 + lane];
-    }
-#pragma unroll
-    for (int c = 0; c < KC2; ++c) w2[c] = u2[(wave * KC2 + c) * 64 + lane];
-#pragma unroll
-    for (int c = 0; c < KC2 / 4; ++c) sw2[c] = s2[(wave * (KC2 / 4) + c) * 64 + lane];
-
     const int64_t step = (int64_t)gridDim.x * ROWS;
-    TileRows<T, D> x;
     int64_t r0 = p.row_begin + (int64_t)blockIdx.x * ROWS;
-    x.load((const T*)p.s, r0, p.row_end);
-    for (; r0 < p.row_end; r0 += step) {
-        x.put(rows);
+    if (wave < 4) {
+        TileRows<T, D, FFN_THREADS / 2> x;
+        x.load(p.s, r0, p.row_end);               // (ahead of the weights: loads return in order)
+        uint4 w1[TILES1][KC];
+        uint32_t sw1[TILES1];
+        const uint4* u1 = (const uint4*)p.w1_packed;
+        const uint32_t* s1 = (const uint32_t*)(u1 + 4 * D / 32 * KC * 64);
+        // Scale word w of a row holds the blocks 8 (w / 2) + w % 2 + 0, 2, 4, 6
+        auto block_of = [&](int i) __attribute__((always_inline)) { const int w = wave * WORDS + i / 4; return w / 2 * 8 + w % 2 + i % 4 * 2; };
+#pragma unroll
+        for (int i = 0; i < TILES1; ++i) {
+#pragma unroll
+            for (int c = 0; c < KC; ++c) w1[i][c] = u1[(block_of(i) * KC + c) * 64 + lane];
+            sw1[i] = s1[block_of(i) * 64 + lane];
+        }
+        auto first = [&](const MxRows<D>& from, MxRows<4 * D>& to) __attribute__((always_inline)) {
+            const uint32_t sb = from.scale(n, hi, 0);
+            uint4 b[KC];
+#pragma unroll
+            for (int c = 0; c < KC; ++c) b[c] = from.operand(n, hi, c);
+#pragma unroll
+            for (int w = 0; w < WORDS; ++w) {
+                uint32_t bytes = 0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int i = 4 * w + j;
+                    f32x16 acc;
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) acc[k] = 0.f;
+                    each<KC>([&](auto c) __attribute__((always_inline)) { mma_mx<c>(w1[i][c], sw1[i], b[c], sb, acc); });
+                    const uint32_t top = block_top<true>(acc), scale = fp4_scale_bits(top);
+                    const uint2 codes = half_codes(acc, scale);
+                    *(uint2*)(to.codes[n] + block_of(i) * 16 + hi * 8) = make_uint2(no_less_than_zero(codes.x), no_less_than_zero(codes.y));
+                    bytes |= (top >= 0x7F800000u ? FP4_BAD : scale >> 23) << (8 * j);
+                }
+                to.scales[wave * WORDS + w][n] = bytes;        // (lane ^ 32 the same)
+            }
+        };
+        x.put(rows[0]);
+        x.keep(full[0]);
+        x.load(p.s, r0 + step, p.row_end);
         __syncthreads();
-        if (r0 + step < p.row_end) x.load((const T*)p.s, r0 + step, p.row_end);
-        const uint32_t sb = rows.scales[n][hi];
+        first(rows[0], hidden[0]);
+        x.put(rows[1]);
+        x.keep(full[1]);
+        x.load(p.s, r0 + 2 * step, p.row_end);
+        int t = 0, t3 = 0;
+        for (; r0 < p.row_end; r0 += step, t ^= 1, t3 = t3 == 2 ? 0 : t3 + 1) {
+            __syncthreads();
+            if (r0 + step < p.row_end) {
+                first(rows[t ^ 1], hidden[t ^ 1]);
+                x.put(rows[t]);
+                x.keep(full[t3 == 0 ? 2 : t3 - 1]);
+                x.load(p.s, r0 + 3 * step, p.row_end);
+            }
+        }
+        __syncthreads();
+    } else {
+        const int quarter = wave - 4;
+        uint4 w2[TILES2][KC2];
+        uint32_t sw2[TILES2][KC2 / 4];
+        const uint4* u2 = (const uint4*)p.w2_packed;
+        const uint32_t* s2 = (const uint32_t*)(u2 + D / 32 * KC2 * 64);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            f32x16 acc;
+        for (int i = 0; i < TILES2; ++i) {
+            const int tile = quarter * TILES2 + i;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) acc[i] = 0.f;
-            each<KC>([&](auto c) __attribute__((always_inline)) {
-                mma_mx<c>(w1[j][c], sw1[j], *(const uint4*)(rows.codes[n] + (2 * c + hi) * 16), sb, acc);
+            for (int c = 0; c < KC2; ++c) w2[i][c] = u2[(tile * KC2 + c) * 64 + lane];
+#pragma unroll
+            for (int c = 0; c < KC2 / 4; ++c) sw2[i][c] = s2[(tile * (KC2 / 4) + c) * 64 + lane];
+        }
+        const int col = quarter * (32 * TILES2) + hi * 16;     // of the first tile's sixteen; the next tile's are 32 further
+        // The activations' first chunks, requested before there is time to wait for them, and their scales
+        constexpr int RING = 4;
+        uint4 ring[RING];
+        uint32_t sb[KC2 / 4];
+        auto request = [&](const MxRows<4 * D>& from) __attribute__((always_inline)) {
+#pragma unroll
+            for (int c = 0; c < KC2 / 4; ++c) sb[c] = from.scale(n, hi, 4 * c);
+#pragma unroll
+            for (int c = 0; c < RING; ++c) ring[c] = from.operand(n, hi, c);
+        };
+        // The row's mean and variance: of the lane's and lane ^ 32's columns; of the row (Chan's update: no difference of large sums).
+        // v: the sums less the wave's mean
+        f32x16 v[TILES2];
+        float mean = 0.f;
+        auto second = [&](const MxRows<4 * D>& from, const FullRows<T, D>& rest, float2 (&to)[4][ROWS]) __attribute__((always_inline)) {
+            f32x16 acc[TILES2];
+#pragma unroll
+            for (int i = 0; i < TILES2; ++i)
+#pragma unroll
+                for (int k = 0; k < 16; ++k) acc[i][k] = 0.f;
+            each<KC2>([&](auto c) __attribute__((always_inline)) {
+#pragma unroll
+                for (int i = 0; i < TILES2; ++i) mma_mx<c>(w2[i][c], sw2[i][c / 4], ring[c % RING], sb[c / 4], acc[i]);
+                if constexpr (c + RING < KC2) ring[c % RING] = from.operand(n, hi, c + RING);
+                __builtin_amdgcn_sched_barrier(0);
             });
-            float v[16];
+            mean = 0.f;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] = acc[i] < 0.f ? 0.f : acc[i];       // (a NaN stays one)
-            uint32_t byte;
-            const int block = 4 * wave + j;
-            *(uint2*)(hidden.codes[n] + block * 16 + hi * 8) = half_block(v, byte);
-            if (hi == 0) *hidden.scale_at(n, block) = (uint8_t)byte;
+            for (int i = 0; i < TILES2; ++i) {
+                float s[16];
+                get16<T>(rest.x[n] + col + 32 * i, s);
+#pragma unroll
+                for (int k = 0; k < 16; ++k) { v[i][k] = s[k] + acc[i][k]; mean += v[i][k]; }
+            }
+            const Pair sums = both_halves(mean);
+            mean = (sums.a + sums.b) * (1.f / (32 * TILES2));
+            float m2 = 0.f;
+#pragma unroll
+            for (int i = 0; i < TILES2; ++i)
+#pragma unroll
+                for (int k = 0; k < 16; ++k) { v[i][k] -= mean; m2 = fmaf(v[i][k], v[i][k], m2); }
+            const Pair squares = both_halves(m2);
+            to[quarter][n] = make_float2(mean, squares.a + squares.b);         // (lane ^ 32 the same)
+        };
+        auto finish = [&](int64_t r0, const float2 (&q)[4]) __attribute__((always_inline)) {
+            const float all = (q[0].x + q[1].x + q[2].x + q[3].x) * 0.25f;
+            float var = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float d = q[i].x - all;
+                var += fmaf((float)(D / 4) * d, d, q[i].y);
+            }
+            const float rstd = rsqrtf(fmaf(var, 1.f / D, p.ln_eps));
+            const float rest = (mean - all) * rstd;
+            const i32x4 tile = tile_buffer<T, D>(p.out, r0, p.row_end);
+#pragma unroll
+            for (int i = 0; i < TILES2; ++i) {
+#pragma unroll
+                for (int k = 0; k < 16; ++k) v[i][k] = fmaf(v[i][k], rstd, rest);
+                put16<T>(tile, (n * D + col + 32 * i) * (int)sizeof(T), v[i]);
+            }
+        };
+        auto parts = [&](const float2 (&from)[4][ROWS], float2 (&q)[4]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) q[i] = from[i][n];
+        };
+        float2 q[4];
+        __syncthreads();
+        int t = 0, t3 = 0;
+        for (; r0 < p.row_end; r0 += step, t ^= 1, t3 = t3 == 2 ? 0 : t3 + 1) {
+            __syncthreads();
+            parts(part[t ^ 1], q);
+            request(hidden[t]);
+            __builtin_amdgcn_sched_barrier(0);
+            if (r0 - step >= p.row_begin) finish(r0 - step, q);
+            second(hidden[t], full[t3], part[t]);
         }
         __syncthreads();
-        f32x16 acc;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) acc[i] = 0.f;
-        each<KC2>([&](auto c) __attribute__((always_inline)) {
-            mma_mx<c>(w2[c], sw2[c / 4], *(const uint4*)(hidden.codes[n] + (2 * c + hi) * 16), hidden.scales[n][c / 4 * 2 + hi], acc);
-        });
-        // The row's mean and variance: of a lane's sixteen columns, of the wave's 32, of the row (Chan's update: no difference of large sums)
-        const int64_t r = min(r0 + n, p.row_end - 1);
-        const int col = wave * 32 + hi * 16;
-        float v[16];
-        get16<T>((const T*)p.s + r * D + col, v);
-        float mean = 0.f, m2 = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) { v[i] += acc[i]; mean += v[i]; }
-        mean += __shfl_xor(mean, 32);
-        mean *= 1.f / 32;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) m2 = fmaf(v[i] - mean, v[i] - mean, m2);
-        m2 += __shfl_xor(m2, 32);
-        if (hi == 0) part[n][wave] = make_float2(mean, m2);
-        __syncthreads();
-        float all = 0.f, var = 0.f;
-#pragma unroll
-        for (int i = 0; i < WAVES; ++i) all += part[n][i].x;
-        all *= 1.f / WAVES;
-#pragma unroll
-        for (int i = 0; i < WAVES; ++i) {
-            const float2 q = part[n][i];
-            var += fmaf(32.f * (q.x - all), q.x - all, q.y);
-        }
-        const float rstd = 1.f / sqrtf(fmaf(var, 1.f / D, p.ln_eps));
-#pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = (v[i] - all) * rstd;
-        if (r0 + n < p.row_end) put16<T>((T*)p.out + r * D + col, v);
+        parts(part[t ^ 1], q);
+        finish(r0 - step, q);
     }
 }
 
@@ -334,7 +491,7 @@ int dg4_launch_mx4_ffn(int dtype, int hidden, const dg4_mx4_ffn_args& a, hipStre
     return by_shape(dtype, hidden, [&](auto t, auto d) {
         using T = decltype(t);
         constexpr int D = d.value;
-        hipLaunchKernelGGL((mx4_ffn_kernel<T, D>), walks(a.row_end - a.row_begin, 256), dim3(2 * D), 0, s, a);
+        hipLaunchKernelGGL((mx4_ffn_kernel<T, D>), walks(a.row_end - a.row_begin, D == 256 ? 256 : 512), dim3(FFN_THREADS), 0, s, a);
         return (int)hipGetLastError();
     });
 }
