@@ -8,6 +8,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <cstring>
 #include <type_traits>
 
 #include "dg4_device.h"
@@ -159,16 +160,17 @@ template <> struct HeadQ<bf16_t> {
     }
     __device__ __forceinline__ bool odd() const
     {
-        constexpr uint16_t low = SMALL_Q >> 16;
-        u16x2 top = { 0, 0 };                     // of the distances above 2^-126; what is below it is far above
-        const u16x2 lows = { low, low };
+        // Twice the bits, which leaves the sign out, less twice 2^-126's: what is below that is far above everything else
+        constexpr uint16_t low = SMALL_Q >> 15;
+        u16x2 top = { 0, 0 };
+        const u16x2 twos = { 2, 2 }, lows = { low, low };
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const uint32_t w[4] = { q[i].x, q[i].y, q[i].z, q[i].w };
 #pragma unroll
-            for (int x = 0; x < 4; ++x) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, w[x] & 0x7FFF7FFFu) - lows);
+            for (int x = 0; x < 4; ++x) top = __builtin_elementwise_max(top, (u16x2)(__builtin_bit_cast(u16x2, w[x]) * twos - lows));
         }
-        return max(top.x, top.y) > (LARGE_Q >> 16) - low;
+        return max(top.x, top.y) > (LARGE_Q >> 15) - low;
     }
     __device__ __forceinline__ float dot(const uint4& w, uint32_t byte) const
     {
@@ -214,7 +216,7 @@ __global__ __launch_bounds__(256) void kv4_attn_kernel(dg4_kv8_attn_args p)
     constexpr int LPR = D / 32, HEADS = D / 32, GPW = 64 / LPR, QUADS = (CH + 3) / 4;
     constexpr int RPW = GPW / S;                  // rows per wave
     constexpr uint32_t NONE = KV4_NEAR_BYTES / D; // past the end of a store that buffer addressing reaches
-    static_assert(S == 1 && ONCE || CH % 4 == 0, "a group's entries are whole pieces of 16 bytes");
+    static_assert((S == 1 && ONCE) || CH == 2 || CH % 4 == 0, "a group's entries are whole pieces");
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int head = lane % LPR, group = lane / LPR, part = group % S;
     // biases of a head by relation code
@@ -233,11 +235,17 @@ __global__ __launch_bounds__(256) void kv4_attn_kernel(dg4_kv8_attn_args p)
     const dg4_i32x4 code_bytes = row_buffer(p.codes, 0, FAR ? 0 : (uint32_t)(p.n * D));
     const dg4_i32x4 scale_bytes = row_buffer(p.scales, 0, FAR ? 0 : (uint32_t)(p.n * 2 * HEADS));
     const uint32_t* erow = p.ell + v * (int64_t)p.ell_w;
-    uint4 ent[QUADS];
+    uint32_t ent[4 * QUADS];
     auto entries = [&](int c0) __attribute__((always_inline)) {
+        using Piece = std::conditional_t<CH == 2, uint2, uint4>;
+        constexpr int E = sizeof(Piece) / 4;
 #pragma unroll
-        for (int i = 0; i < QUADS; ++i)
-            ent[i] = c0 + 4 * i < p.ell_w ? *(const uint4*)(erow + c0 + 4 * i) : make_uint4(DG4_ELL_PAD, DG4_ELL_PAD, DG4_ELL_PAD, DG4_ELL_PAD);
+        for (int i = 0; i < (CH + E - 1) / E; ++i) {
+            Piece e;
+            if (c0 + E * i < p.ell_w) e = *(const Piece*)(erow + c0 + E * i);
+            else memset(&e, 0xFF, sizeof(e));
+            memcpy(ent + E * i, &e, sizeof(e));
+        }
     };
     entries(part * CH);
     HeadQ<T> q;
@@ -255,13 +263,13 @@ __global__ __launch_bounds__(256) void kv4_attn_kernel(dg4_kv8_attn_args p)
         for (int i = 0; i < 32; ++i) acc[i] = 0.f;
     }
     for (int c0 = part * CH; ONCE || c0 < p.ell_w; c0 += S * CH) {
-        if (!ONCE && ent[0].x == DG4_ELL_PAD) break;           // padding stands at the end only; the same for all lanes of the group
+        if (!ONCE && ent[0] == DG4_ELL_PAD) break;           // padding stands at the end only; the same for all lanes of the group
         uint4 kw[CH], vw[CH];
         uint32_t sw[CH];                          // scales: of K, and of V from bit 8
         float b[CH];
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
-            const uint32_t e = j % 4 == 0 ? ent[j / 4].x : j % 4 == 1 ? ent[j / 4].y : j % 4 == 2 ? ent[j / 4].z : ent[j / 4].w;
+            const uint32_t e = ent[j];
             const float bj = bias[head][e >> 30];
             b[j] = e == DG4_ELL_PAD ? -INFINITY : bj;
             const bool none = b[j] == -INFINITY;
@@ -423,7 +431,7 @@ int launch_attn_of(const dg4_kv8_attn_args& args, hipStream_t s)
     constexpr int GPW = 64 / (D / 32);
     constexpr bool ONCE = MOST <= 15;
     constexpr int S = MOST <= 7 ? 1 : MOST <= 31 ? 2 : MOST <= 127 ? 4 : MOST <= 255 ? 8 : GPW;
-    constexpr int CH = MOST <= 7 ? MOST : ONCE ? 8 : 4;
+    constexpr int CH = MOST <= 7 ? MOST : ONCE ? 8 : 2;
     return launch_rows(args, 4 * GPW / S, [&](const dg4_kv8_attn_args& a, dim3 grid) {
         hipLaunchKernelGGL((kv4_attn_kernel<T, D, S, CH, ONCE, FAR>), grid, dim3(256), 0, s, a);
     });

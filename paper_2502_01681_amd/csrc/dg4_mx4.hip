@@ -92,6 +92,7 @@ template <typename T, int D> struct FullRows { T x[ROWS][D + 16 / (int)sizeof(T)
 // Rows of a tile as a buffer: what lies behind the call's last row reads as zeros and is not written, without a branch (behind
 // which a wait for loads would be one for every store before it, too). No rows at all (r0 past the end, or not yet there): nothing.
 typedef int i32x4 __attribute__((ext_vector_type(4)));
+constexpr int PAST_CACHES = 2;                    // a buffer store's cache policy: non-temporal
 __device__ i32x4 dg4_raw_buffer_load16(i32x4 rsrc, int voffset, int soffset, int aux) __asm("llvm.amdgcn.raw.buffer.load.v4i32");
 __device__ void dg4_raw_buffer_store16(i32x4 v, i32x4 rsrc, int voffset, int soffset, int aux) __asm("llvm.amdgcn.raw.buffer.store.v4i32");
 template <typename T, int D> __device__ __forceinline__ i32x4 tile_buffer(const void* rows, int64_t r0, int64_t r_end)
@@ -197,35 +198,22 @@ template <typename T> __device__ __forceinline__ void get16(const T* from, float
     }
 }
 
-template <typename T> __device__ __forceinline__ void put16(i32x4 tile, int at, const f32x16& v)
-{
-    float x[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = v[i];
-    if constexpr (sizeof(T) == 2) {
-        uint4 a, b;
-        Elem<bf16_t>::pack(x, a, b);
-        dg4_raw_buffer_store16(__builtin_bit_cast(i32x4, a), tile, at, 0, 0);
-        dg4_raw_buffer_store16(__builtin_bit_cast(i32x4, b), tile, at + 16, 0, 0);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const i32x4 w = { (int)__float_as_uint(x[4 * i]), (int)__float_as_uint(x[4 * i + 1]), (int)__float_as_uint(x[4 * i + 2]), (int)__float_as_uint(x[4 * i + 3]) };
-            dg4_raw_buffer_store16(w, tile, at + 16 * i, 0, 0);
-        }
-    }
-}
-
 // A workgroup has a wave for every head, whose columns of Wq, Wk and Wv stay in its registers, and takes tiles of rows in turn: the
-// rows of the next tile travel while this one is multiplied.
+// rows of the next tile travel while this one is multiplied. Results leave by way of LDS, so that a store is whole rows.
 template <typename T, int D, bool STORE>
 __global__ __launch_bounds__(2 * D) void mx4_proj_kernel(dg4_mx4_proj_args p)
 {
-    constexpr int HEADS = D / 32, KC = D / 64;
+    constexpr int HEADS = D / 32, KC = D / 64, OUTS = STORE ? 1 : 3;
     __shared__ MxRows<D> rows[2];
+    __shared__ FullRows<T, D> outs[OUTS];
+    __shared__ uint8_t codes[STORE ? ROWS : 1][D + 16], scales[STORE ? ROWS : 1][2 * HEADS];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 31, hi = lane >> 5;
+    const int64_t step = (int64_t)gridDim.x * ROWS;
+    TileRows<T, D, 2 * D> x;
+    int64_t r0 = p.row_begin + (int64_t)blockIdx.x * ROWS;
+    x.load(p.s, r0, p.row_end);                   // (ahead of the weights: loads return in order)
     uint4 w[3][KC];
     uint32_t sw[3];
 #pragma unroll
@@ -235,39 +223,49 @@ __global__ __launch_bounds__(2 * D) void mx4_proj_kernel(dg4_mx4_proj_args p)
         for (int c = 0; c < KC; ++c) w[j][c] = ((const uint4*)p.w_packed)[(tile * KC + c) * 64 + lane];
         sw[j] = ((const uint32_t*)((const uint4*)p.w_packed + 3 * D / 32 * KC * 64))[tile * 64 + lane];
     }
-    const int64_t step = (int64_t)gridDim.x * ROWS;
-    TileRows<T, D, 2 * D> x;
-    int64_t r0 = p.row_begin + (int64_t)blockIdx.x * ROWS;
-    x.load(p.s, r0, p.row_end);
     for (int t = 0; r0 < p.row_end; r0 += step, t ^= 1) {
         x.put(rows[t]);
         __syncthreads();
         x.load(p.s, r0 + step, p.row_end);
-        f32x16 acc[3];
-#pragma unroll
-        for (int j = 0; j < 3; ++j)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[j][i] = 0.f;
         const uint32_t sb = rows[t].scale(n, hi, 0);
-        each<KC>([&](auto c) __attribute__((always_inline)) {
-            const uint4 b = rows[t].operand(n, hi, c);
+        uint4 b[KC];
 #pragma unroll
-            for (int j = 0; j < 3; ++j) mma_mx<c>(w[j][c], sw[j], b, sb, acc[j]);
-        });
-        const int64_t r = r0 + n;
-        int64_t at = -1;
-        if (r < p.row_end) at = STORE && p.ids ? (int64_t)p.ids[r] : r;
+        for (int c = 0; c < KC; ++c) b[c] = rows[t].operand(n, hi, c);
 #pragma unroll
         for (int j = 0; j < 3; ++j) {
-            if (STORE && j > 0) {
-                const uint32_t byte = fp4_scale_byte(block_top<false>(acc[j]));
-                const uint2 codes = byte == FP4_BAD ? make_uint2(0, 0) : half_codes(acc[j], byte << 23);
-                if (at >= 0 && at < p.n_store) {
-                    *(uint2*)(p.codes + at * D + (j - 1) * (D / 2) + wave * 16 + hi * 8) = codes;
-                    if (hi == 0) p.scales[(at * HEADS + wave) * 2 + j - 1] = (uint8_t)byte;
+            f32x16 acc;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[i] = 0.f;
+            each<KC>([&](auto c) __attribute__((always_inline)) { mma_mx<c>(w[j][c], sw[j], b[c], sb, acc); });
+            if constexpr (STORE) {
+                if (j > 0) {
+                    const uint32_t byte = fp4_scale_byte(block_top<false>(acc));
+                    *(uint2*)(codes[n] + (j - 1) * (D / 2) + wave * 16 + hi * 8) = byte == FP4_BAD ? make_uint2(0, 0) : half_codes(acc, byte << 23);
+                    scales[n][wave * 2 + j - 1] = (uint8_t)byte;               // (lane ^ 32 the same)
+                    continue;
                 }
-            } else if (r < p.row_end) {
-                put16<T>((T*)p.out[j] + r * D + wave * 32 + hi * 16, acc[j]);
+            }
+            put16<T>(outs[STORE ? 0 : j].x[n] + wave * 32 + hi * 16, acc);
+        }
+        __syncthreads();
+        constexpr int PPR = D * (int)sizeof(T) / 16, PIECES = ROWS * PPR / (2 * D);
+#pragma unroll
+        for (int j = 0; j < OUTS; ++j) {
+            const i32x4 tile = tile_buffer<T, D>(p.out[j], r0, p.row_end);
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {
+                const int piece = (int)threadIdx.x + 2 * D * i;
+                dg4_raw_buffer_store16(__builtin_bit_cast(i32x4, *((const uint4*)outs[j].x[piece / PPR] + piece % PPR)), tile, piece * 16, 0, PAST_CACHES);
+            }
+        }
+        if constexpr (STORE) {
+            const int row = (int)threadIdx.x / (D / 16), piece = (int)threadIdx.x % (D / 16);
+            const int64_t r = r0 + row;
+            int64_t at = -1;
+            if (r < p.row_end) at = p.ids ? (int64_t)p.ids[r] : r;
+            if (at >= 0 && at < p.n_store) {
+                *(uint4*)(p.codes + at * D + piece * 16) = *(const uint4*)(codes[row] + piece * 16);
+                if (piece < HEADS / 4) *(uint2*)(p.scales + at * (2 * HEADS) + piece * 8) = *(const uint2*)(scales[row] + piece * 8);
             }
         }
     }
@@ -293,6 +291,8 @@ __global__ __launch_bounds__(FFN_THREADS) void mx4_ffn_kernel(dg4_mx4_ffn_args p
     __shared__ MxRows<4 * D> hidden[2];
     __shared__ FullRows<T, D> full[3];
     __shared__ float2 part[2][4][ROWS];
+    constexpr int OUT_ROWS = sizeof(T) == 2 ? ROWS : 8;       // (what LDS has room for)
+    __shared__ __align__(16) T outs[4][OUT_ROWS][32 * TILES2 + 16 / (int)sizeof(T)];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 31, hi = lane >> 5;
@@ -426,10 +426,26 @@ __global__ __launch_bounds__(FFN_THREADS) void mx4_ffn_kernel(dg4_mx4_ffn_args p
             const float rest = (mean - all) * rstd;
             const i32x4 tile = tile_buffer<T, D>(p.out, r0, p.row_end);
 #pragma unroll
-            for (int i = 0; i < TILES2; ++i) {
+            for (int i = 0; i < TILES2; ++i)
 #pragma unroll
                 for (int k = 0; k < 16; ++k) v[i][k] = fmaf(v[i][k], rstd, rest);
-                put16<T>(tile, (n * D + col + 32 * i) * (int)sizeof(T), v[i]);
+            // OUT_ROWS rows at a time through the wave's own LDS (a wave's LDS operations complete in order), so that lanes side by side store
+            // pieces side by side
+            constexpr int PPR = 2 * TILES2 * (int)sizeof(T), PIECES = OUT_ROWS * PPR / 64;             // pieces of 16 bytes: of the wave's part of a row, of a lane
+#pragma unroll
+            for (int r = 0; r < ROWS; r += OUT_ROWS) {
+                if (OUT_ROWS == ROWS || n / OUT_ROWS * OUT_ROWS == r) {
+#pragma unroll
+                    for (int i = 0; i < TILES2; ++i) put16<T>(outs[quarter][n % OUT_ROWS] + 32 * i + hi * 16, v[i]);
+                }
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+                for (int i = 0; i < PIECES; ++i) {
+                    const int piece = lane + 64 * i, row = piece / PPR;
+                    const uint4 x = *((const uint4*)outs[quarter][row] + piece % PPR);
+                    dg4_raw_buffer_store16(__builtin_bit_cast(i32x4, x), tile, (r + row) * (D * (int)sizeof(T)) + (quarter * PPR + piece % PPR) * 16, 0, PAST_CACHES);
+                }
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             }
         };
         auto parts = [&](const float2 (&from)[4][ROWS], float2 (&q)[4]) __attribute__((always_inline)) {
@@ -480,7 +496,7 @@ int dg4_launch_mx4_proj(int dtype, int hidden, const dg4_mx4_proj_args& a, hipSt
     return by_shape(dtype, hidden, [&](auto t, auto d) {
         using T = decltype(t);
         constexpr int D = d.value;
-        const dim3 grid = walks(a.row_end - a.row_begin, 512);
+        const dim3 grid = walks(a.row_end - a.row_begin, D == 256 ? 256 : 512);
         if (a.codes) hipLaunchKernelGGL((mx4_proj_kernel<T, D, true>), grid, dim3(2 * D), 0, s, a);
         else hipLaunchKernelGGL((mx4_proj_kernel<T, D, false>), grid, dim3(2 * D), 0, s, a);
         return (int)hipGetLastError();

@@ -149,9 +149,9 @@ def close(A, want, bound):
 
 @pytest.mark.parametrize("hidden", [128, 256])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("n,hops", [(230, 1), (230, 2), (230, 3), (150, 4), (200, 5), (330, 8)])
+@pytest.mark.parametrize("n,hops", [(230, 1), (230, 2), (230, 3), (150, 4), (200, 5), (260, 6), (300, 7), (330, 8)])
 def test_attention(hidden, dtype, n, hops):
-    g = circuit(n, 24 if hops < 8 else 330, hops)
+    g = circuit(n, 24 if hops < 6 else 330, hops)
     print(f"kv4 attention {hidden} {dtype} n={n} hops={hops} longest row {int(np.diff(g.array('nbr_ptr')).max())}", flush=True)
     codes, scales = store(3, n, hidden)
     rng = np.random.default_rng(4)
