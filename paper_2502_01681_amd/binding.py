@@ -1,4 +1,4 @@
-"""ctypes binding of libdg4.so: argument marshalling only."""
+"""Binding of libdg4.so by ctypes, for the calls in 4 bits by a module of its own (csrc/dg4_marshal.cpp): argument marshalling only."""
 from __future__ import annotations
 
 import ctypes
@@ -390,9 +390,9 @@ def _call(where: str, cfg: LayerConfig, first):
     return _types[cfg.dtype], dev, _raw_stream(dev)
 
 
-def _shape(cfg: LayerConfig, ln_eps=0.0):
+def _shape(cfg: LayerConfig):
     """What the serving calls look at of a configuration, for the C call (its flags are dg4_layer_fwd's)."""
-    return ctypes.byref(_Cfg(cfg.hidden, cfg.heads, cfg.hops, 1, DG4_F32 if cfg.dtype == "f32" else DG4_BF16, 0, ln_eps))
+    return ctypes.byref(_Cfg(cfg.hidden, cfg.heads, cfg.hops, 1, DG4_F32 if cfg.dtype == "f32" else DG4_BF16))
 
 
 @dataclass
@@ -451,20 +451,15 @@ def dg4_qkv_proj_lora(cfg: LayerConfig, weights: LoraWeights, S, adapter, Q, K, 
     _check(rc, where)
 
 
-_IN_4_BITS = object()            # _store_call's fmt for a store in 4 bits
-
-
-def _store_call(where: str, cfg: LayerConfig, fmt, codes, scales, ids, x, y, row_begin, row_end):
-    """What the calls on a K|V store in 8 or 4 bits check and fill in, for rows x and y beside it: (format or, with nothing to
+def _store_call(where: str, cfg: LayerConfig, fmt: str, codes, scales, ids, x, y, row_begin, row_end):
+    """What the calls on a K|V store in 8 bits check and fill in, for rows x and y beside it: (format or, with nothing to
     do, None; end of the range; store rows; address of ids; stream)."""
     td, dev, stream = _call(where, cfg, codes)
     n, rows = codes.shape[0], x.shape[0]
     row_end = rows if row_end is None else row_end
-    four = fmt is _IN_4_BITS
     k, byte = rows * cfg.hidden, _types["bytes"]               # (_refused of each, without the calls: a level's call is short)
-    if (not (four or fmt in KV_FORMATS) or row_end > rows or x.dtype is not td or y.dtype is not td or codes.dtype is not byte or
-            scales.dtype is not byte or x.numel() != k or y.numel() != k or
-            codes.numel() != (n if four else 2 * n) * cfg.hidden or
+    if (fmt not in KV_FORMATS or row_end > rows or x.dtype is not td or y.dtype is not td or codes.dtype is not byte or
+            scales.dtype is not byte or x.numel() != k or y.numel() != k or codes.numel() != n * 2 * cfg.hidden or
             scales.shape != (n, cfg.heads, 2) or not (x.is_contiguous() and y.is_contiguous() and codes.is_contiguous() and
                                                       scales.is_contiguous()) or
             x.get_device() != dev or y.get_device() != dev or scales.get_device() != dev or
@@ -472,7 +467,7 @@ def _store_call(where: str, cfg: LayerConfig, fmt, codes, scales, ids, x, y, row
         raise DG4Error(-1, where)
     if row_begin == row_end == 0 or n == 0 and ids is not None:      # (an empty tensor has no address)
         return None, 0, n, None, stream
-    return 4 if four else KV_FORMATS[fmt], row_end, n, ids.data_ptr() if ids is not None else None, stream
+    return KV_FORMATS[fmt], row_end, n, ids.data_ptr() if ids is not None else None, stream
 
 
 def dg4_kv8_write(cfg: LayerConfig, fmt: str, K, V, codes, scales, ids=None, row_begin=0, row_end=None):
@@ -510,39 +505,42 @@ def dg4_sparse_attn_kv8_fwd(cfg: LayerConfig, fmt: str, g: Graph, Q, codes, scal
     _check(rc, "dg4_sparse_attn_kv8_fwd")
 
 
+_marshal_module = None
+
+
+def _marshal():
+    """Checks of arguments and the C calls of the functions below, natively: their calls are as short as a look at ten tensors."""
+    global _marshal_module
+    if _marshal_module is None:
+        import importlib.machinery
+        import importlib.util
+        import torch
+        if not os.path.exists(_build.MARSHAL):
+            _build.build(force=False)
+        loader = importlib.machinery.ExtensionFileLoader("_dg4_marshal", _build.MARSHAL)
+        m = importlib.util.module_from_spec(importlib.util.spec_from_file_location("_dg4_marshal", _build.MARSHAL, loader=loader))
+        loader.exec_module(m)
+        names = ("dg4_kv4_write", "dg4_kv4_read", "dg4_sparse_attn_kv4_fwd", "dg4_qkv_proj_mx4", "dg4_qkv_proj_kv4", "dg4_ffn_mx4_fwd")
+        m.bind(*(ctypes.cast(getattr(lib(), n), _P).value for n in names), DG4Error, torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice)
+        _marshal_module = m              # (last: another thread's first call goes by this one)
+    return _marshal_module
+
+
 def dg4_kv4_write(cfg: LayerConfig, K, V, codes, scales, ids=None, row_begin=0, row_end=None):
     """Rows [row_begin,row_end) of K and V into the store in 4 bits: codes uint8 [n, hidden] and scales uint8 [n, heads, 2] in
     place. ids: int32 store row of each row (outside the store: skipped), else the row itself; a store row that is named twice
     holds neither row whole."""
-    f, row_end, n, ip, stream = _store_call("dg4_kv4_write", cfg, _IN_4_BITS, codes, scales, ids, K, V, row_begin, row_end)
-    if f is None:
-        return
-    rc = lib().dg4_kv4_write(_shape(cfg), K.data_ptr(), V.data_ptr(), row_begin, row_end, ip, codes.data_ptr(),
-                             scales.data_ptr(), n, stream)
-    _check(rc, "dg4_kv4_write")
+    (_marshal_module or _marshal()).kv4_write(cfg, K, V, codes, scales, ids, row_begin, row_end)
 
 
 def dg4_kv4_read(cfg: LayerConfig, codes, scales, K, V, ids=None, row_begin=0, row_end=None):
     """Rows [row_begin,row_end) of K and V, in place, from the store in 4 bits; ids as in dg4_kv4_write."""
-    f, row_end, n, ip, stream = _store_call("dg4_kv4_read", cfg, _IN_4_BITS, codes, scales, ids, K, V, row_begin, row_end)
-    if f is None:
-        return
-    rc = lib().dg4_kv4_read(_shape(cfg), codes.data_ptr(), scales.data_ptr(), n, ip, row_begin, row_end,
-                            K.data_ptr(), V.data_ptr(), stream)
-    _check(rc, "dg4_kv4_read")
+    (_marshal_module or _marshal()).kv4_read(cfg, codes, scales, K, V, ids, row_begin, row_end)
 
 
 def dg4_sparse_attn_kv4_fwd(cfg: LayerConfig, g: Graph, Q, codes, scales, rel_bias, A, ids=None, row_begin=0, row_end=None):
     """Cone attention over the store in 4 bits (row = node id). ids: int32 gate of each row of Q and A, else the row itself."""
-    where = "dg4_sparse_attn_kv4_fwd"
-    f, row_end, n, ip, stream = _store_call(where, cfg, _IN_4_BITS, codes, scales, ids, Q, A, row_begin, row_end)
-    if n < g.n or _refused(rel_bias, _types["f32"], codes.get_device(), 4 * cfg.heads):
-        raise DG4Error(-1, where)
-    if f is None:
-        return
-    rc = lib().dg4_sparse_attn_kv4_fwd(_shape(cfg), g.handle, row_begin, row_end, ip, Q.data_ptr(), codes.data_ptr(),
-                                       scales.data_ptr(), rel_bias.data_ptr(), A.data_ptr(), stream)
-    _check(rc, where)
+    (_marshal_module or _marshal()).sparse_attn_kv4_fwd(cfg, g._h.value, g.n, Q, codes, scales, rel_bias, A, ids, row_begin, row_end)
 
 
 @dataclass
@@ -574,54 +572,20 @@ def dg4_mx4_pack(cfg: LayerConfig, W) -> Mx4Weights:
     return Mx4Weights(packed, k, n, cfg.hidden)
 
 
-def _mx4_refused(weights: Mx4Weights, cfg: LayerConfig, dev, k, n) -> bool:
-    return weights.hidden != cfg.hidden or weights.k != k or weights.n != n or weights.packed.get_device() != dev
-
-
 def dg4_qkv_proj_mx4(cfg: LayerConfig, weights: Mx4Weights, S, Q, K, V, row_begin=0, row_end=None):
     """Q, K, V rows [row_begin,row_end) = S rows x Wqkv, both in blocks of 4 bits. In place."""
-    where, d, rows = "dg4_qkv_proj_mx4", cfg.hidden, S.shape[0]
-    td, dev, stream = _call(where, cfg, S)
-    row_end = rows if row_end is None else row_end
-    if (row_end > rows or _mx4_refused(weights, cfg, dev, d, 3 * d) or _refused(S, td, dev, rows * d) or
-            _refused(Q, td, dev, rows * d) or _refused(K, td, dev, rows * d) or _refused(V, td, dev, rows * d)):
-        raise DG4Error(-1, where)
-    if row_begin == row_end == 0:                # (an empty tensor has no address)
-        return
-    packed = weights.packed
-    rc = lib().dg4_qkv_proj_mx4(_shape(cfg), packed.data_ptr(), packed.numel(), S.data_ptr(), row_begin, row_end,
-                                Q.data_ptr(), K.data_ptr(), V.data_ptr(), stream)
-    _check(rc, where)
+    (_marshal_module or _marshal()).qkv_proj_mx4(cfg, weights, S, Q, K, V, row_begin, row_end)
 
 
 def dg4_qkv_proj_kv4(cfg: LayerConfig, weights: Mx4Weights, S, Q, codes, scales, ids=None, row_begin=0, row_end=None):
-    """dg4_qkv_proj_mx4 with K and V straight into the store in 4 bits (codes, scales, ids as in dg4_kv4_write). In place."""
-    where, d = "dg4_qkv_proj_kv4", cfg.hidden
-    f, end, n, ip, stream = _store_call(where, cfg, _IN_4_BITS, codes, scales, ids, S, Q, row_begin, row_end)
-    # (a store without rows has no address, and rows of Q would have to be written all the same)
-    if _mx4_refused(weights, cfg, codes.get_device(), d, 3 * d) or f is None and n == 0 and S.shape[0]:
-        raise DG4Error(-1, where)
-    if f is None:
-        return
-    packed = weights.packed
-    rc = lib().dg4_qkv_proj_kv4(_shape(cfg), packed.data_ptr(), packed.numel(), S.data_ptr(), row_begin, end, ip,
-                                Q.data_ptr(), codes.data_ptr(), scales.data_ptr(), n, stream)
-    _check(rc, where)
+    """dg4_qkv_proj_mx4 with K and V straight into the store in 4 bits (codes, scales, ids as in dg4_kv4_write; the store has a row). In
+    place."""
+    (_marshal_module or _marshal()).qkv_proj_kv4(cfg, weights, S, Q, codes, scales, ids, row_begin, row_end)
 
 
 def dg4_ffn_mx4_fwd(cfg: LayerConfig, W1: Mx4Weights, W2: Mx4Weights, S, Out, row_begin=0, row_end=None):
     """Out rows [row_begin,row_end) = LayerNorm(S + relu(S W1) W2), products in blocks of 4 bits. In place."""
-    where, d, rows = "dg4_ffn_mx4_fwd", cfg.hidden, S.shape[0]
-    td, dev, stream = _call(where, cfg, S)
-    row_end = rows if row_end is None else row_end
-    if (row_end > rows or _mx4_refused(W1, cfg, dev, d, 4 * d) or _mx4_refused(W2, cfg, dev, 4 * d, d) or
-            _refused(S, td, dev, rows * d) or _refused(Out, td, dev, rows * d)):
-        raise DG4Error(-1, where)
-    if row_begin == row_end == 0:                # (an empty tensor has no address)
-        return
-    rc = lib().dg4_ffn_mx4_fwd(_shape(cfg, cfg.ln_eps), W1.packed.data_ptr(), W1.packed.numel(), W2.packed.data_ptr(),
-                               W2.packed.numel(), S.data_ptr(), row_begin, row_end, Out.data_ptr(), stream)
-    _check(rc, where)
+    (_marshal_module or _marshal()).ffn_mx4_fwd(cfg, W1, W2, S, Out, row_begin, row_end)
 
 
 def dg4_layer_fwd(cfg: LayerConfig, g: Graph, X, weights, Hout, level_begin=0, level_end=None, workspace=None):

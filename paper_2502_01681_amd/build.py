@@ -1,18 +1,23 @@
-"""Build libdg4.so (HIP kernels + C ABI) in-tree for gfx950."""
+"""Build libdg4.so (HIP kernels + C ABI) in-tree for gfx950, and the native part of the Python binding."""
 from __future__ import annotations
 
+import importlib.util
 import os
 import subprocess
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdg4.so")
+MARSHAL = os.path.join(HERE, "_dg4_marshal.so")
 OBJ = os.path.join(HERE, "_build")
 SOURCES = ["dg4_graph.cpp", "dg4_graph_gpu.hip", "dg4_api.cpp", "dg4_kernels.hip", "dg4_sweep.hip", "dg4_flow.hip", "dg4_heads.hip",
            "dg4_static.hip", "dg4_kv8.hip", "dg4_lora.hip", "dg4_kv4.hip", "dg4_mx4.hip"]
 HEADERS = [os.path.join(CSRC, h) for h in ("dg4_internal.h", "dg4_device.h", "dg4_rowops.h", "dg4_wait.h", "dg4_fp4.h")] + [os.path.join(ROOT, "include", h) for h in ("dg4.h", "dg4_serving.h", "dg4_mx4.h")]
+
+MARSHAL_SOURCE = os.path.join(CSRC, "dg4_marshal.cpp")
 
 
 def sources():
@@ -20,10 +25,10 @@ def sources():
 
 
 def stale() -> bool:
-    if not os.path.exists(LIB):
+    if not os.path.exists(LIB) or not os.path.exists(MARSHAL):
         return True
-    t = os.path.getmtime(LIB)
-    return any(os.path.getmtime(d) > t for d in sources() + HEADERS)
+    t = min(os.path.getmtime(LIB), os.path.getmtime(MARSHAL))
+    return any(os.path.getmtime(d) > t for d in sources() + HEADERS + [MARSHAL_SOURCE])
 
 
 def _flags():
@@ -38,6 +43,14 @@ def _flags():
             "-mllvm", "-amdgpu-atomic-optimizer-strategy=None",
             "-I", os.path.join(ROOT, "include"), "-I", CSRC,
             "-Wall", "-Wno-unused-function"]
+
+
+def _build_marshal():
+    """The native part of the Python binding (host code, against this interpreter and torch)."""
+    torch = os.path.dirname(importlib.util.find_spec("torch").origin)
+    subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-I", sysconfig.get_paths()["include"],
+                           "-isystem", os.path.join(torch, "include"), "-I", os.path.join(ROOT, "include"), MARSHAL_SOURCE, "-o", MARSHAL,
+                           "-L", os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"])
 
 
 def build(force: bool = True) -> str:
@@ -57,7 +70,10 @@ def build(force: bool = True) -> str:
         return obj
 
     with ThreadPoolExecutor(max_workers=min(8, len(SOURCES))) as ex:
+        marshal = ex.submit(_build_marshal) if force or not os.path.exists(MARSHAL) or os.path.getmtime(MARSHAL) < max(os.path.getmtime(MARSHAL_SOURCE), newest_header) else None
         objs = list(ex.map(compile_one, sources()))
+        if marshal is not None:
+            marshal.result()
     subprocess.check_call([hipcc, "-shared", "-fPIC", "--offload-arch=gfx950", "-o", LIB] + objs)
     return LIB
 

@@ -148,3 +148,41 @@ def test_binding_turns_away_what_is_not_on_the_device():
                  lambda: dg4.dg4_qkv_proj_kv4(cfg(), w, x, x, codes, scales), lambda: dg4.dg4_ffn_mx4_fwd(cfg(), w, w, x, x)):
         with pytest.raises(dg4.DG4Error):
             call()
+
+
+def test_binding_turns_away_what_is_no_tensor_or_no_configuration():
+    import torch
+    x, codes, scales = torch.zeros((3, 128)), torch.zeros((3, 128), dtype=torch.uint8), torch.zeros((3, 4, 2), dtype=torch.uint8)
+    for call in (lambda: dg4.dg4_kv4_write(cfg(), None, x, codes, scales), lambda: dg4.dg4_kv4_read(cfg(), np.zeros(3), scales, x, x),
+                 lambda: dg4.dg4_kv4_write(cfg(dtype=1), x, x, codes, scales), lambda: dg4.dg4_kv4_write(cfg(dtype="f16"), x, x, codes, scales),
+                 lambda: dg4.dg4_kv4_write(cfg(), torch.zeros(()), x, codes, scales), lambda: dg4.dg4_ffn_mx4_fwd(cfg(), None, None, "S", x)):
+        with pytest.raises(dg4.DG4Error):
+            call()
+    for call in (lambda: dg4.dg4_kv4_write(None, x, x, codes, scales), lambda: dg4.dg4_kv4_write(cfg(), x, x, codes), lambda: dg4.dg4_kv4_write(cfg(), x, x, codes, scales, row=3)):
+        with pytest.raises((AttributeError, TypeError)):
+            call()
+
+
+def test_two_threads_make_the_first_call_of_a_process():
+    """In a process of its own: the binding's native part is loaded by whoever comes first, and both calls get their answer."""
+    import subprocess
+    import sys
+    code = """
+import threading
+import torch
+import paper_2502_01681_amd as dg4
+cfg = dg4.LayerConfig(128, 4, 2, 1, "f32")
+x, codes, scales = torch.zeros((3, 128)), torch.zeros((3, 128), dtype=torch.uint8), torch.zeros((3, 4, 2), dtype=torch.uint8)
+got, go = [], threading.Barrier(4)
+def run():
+    go.wait()
+    try:
+        dg4.dg4_kv4_write(cfg, x, x, codes, scales)
+    except dg4.DG4Error as e:
+        got.append(e.name)
+threads = [threading.Thread(target=run) for _ in range(4)]
+[t.start() for t in threads]
+[t.join() for t in threads]
+assert got == ["EINVAL"] * 4, got
+"""
+    subprocess.run([sys.executable, "-c", code], check=True, cwd=os.path.join(os.path.dirname(__file__), ".."), timeout=120)
