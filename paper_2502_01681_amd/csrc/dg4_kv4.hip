@@ -21,8 +21,9 @@ namespace {
 // Bytes of codes up to which buffer addressing is used: offsets are 32 bits, and there is room for one that is past the end
 constexpr uint32_t KV4_NEAR_BYTES = 0xC0000000u;
 
-// Which run of rows a workgroup takes. Workgroups go to the eight XCDs in turn, and neighbouring rows read the same sources:
-// runs of 128 workgroups go to one XCD, so that its L2 serves them. What is left behind the last eight whole runs goes in turn.
+// Which run of rows a workgroup takes. Workgroups go to the eight XCDs in turn, and neighbouring rows read the same sources: runs of 64
+// workgroups (2048 rows of two hops at hidden 256) go to one XCD, so that its L2 serves them. (A million rows, runs of 16, 32, 64 and 128:
+// 311, 300, 299 and 302 us.) What is left behind the last eight whole runs goes in turn.
 __device__ __forceinline__ uint32_t kv4_block(uint32_t block, uint32_t blocks)
 {
     constexpr uint32_t RUN = 64;
@@ -31,7 +32,9 @@ __device__ __forceinline__ uint32_t kv4_block(uint32_t block, uint32_t blocks)
 }
 
 // A lane takes eight features, so a block is four lanes and a gate's K | V row a whole wave at hidden 256 (two gates at 128).
-// U gates per lane, all requested before the first is used.
+// U gates per lane, all requested before the first is used. Bound by HBM: 1, 2, 4 and 8 gates per lane take 216, 215, 227 and 232 us for a
+// million rows of bfloat16 at hidden 256 (1.30 GB moved, 6.0 TB/s), 160, 169, 175 and 176 for 402,193 of fp32 and 2.1, 2.2, 2.5 and 3.1 for 264 of
+// bfloat16: two of bfloat16, one of fp32. Codes leave through the caches, where the next level's attention finds them (past them: 209).
 template <typename T, int D, int U>
 __global__ __launch_bounds__(256) void kv4_write_kernel(dg4_kv8_args p)
 {
@@ -66,7 +69,9 @@ __global__ __launch_bounds__(256) void kv4_write_kernel(dg4_kv8_args p)
     }
 }
 
-// A lane takes what it stores as 16 bytes, so that a wave's store is whole lines: four features of fp32, eight of bfloat16. U rows per lane.
+// A lane takes what it stores as 16 bytes, so that a wave's store is whole lines: four features of fp32, eight of bfloat16. U rows per lane:
+// 232, 204 and 222 us with 1, 2 and 4 for a million rows of bfloat16 at hidden 256 (1.30 GB moved, 6.4 TB/s; 215 where rows leave through the
+// caches), 128, 128 and 145 for 402,193 of fp32 (149).
 template <typename T, int D, int U>
 __global__ __launch_bounds__(256) void kv4_read_kernel(dg4_kv8_args p)
 {
@@ -205,11 +210,17 @@ template <> struct HeadQ<bf16_t> {
 };
 
 // A lane owns a head of a destination row, a row is S groups of D / 32 lanes: a source's K codes are one load instruction over
-// a whole line, its V codes another. The row's entries go to the groups in turn, CH at a time; each group keeps a running maximum,
-// denominator and weighted sum (32 bits), joined at the end by lane exchange. ONCE: the groups take the whole row at one go.
-// Entries that are none (padding, a relation whose bias is -inf) ask the buffers for an offset past the end: zeros, no request, no
-// branch, and what the store holds there cannot matter. The offsets of buffer addressing are 32 bits: FAR, for larger stores, has
-// addresses of 64 bits and reads zeros from memory for them.
+// a whole line, its V codes another, and a score needs no other lane. The row's entries go to the groups in turn, CH at a time; each
+// group keeps a running maximum, denominator and weighted sum (32 bits), joined at the end by lane exchange. ONCE: the groups take the
+// whole row at one go. Entries that are none (padding, a relation whose bias is -inf) ask the buffers for an offset past the end: zeros, no
+// request, no branch, and what the store holds there cannot matter. The offsets of buffer addressing are 32 bits: FAR, for larger stores,
+// has addresses of 64 bits and reads zeros from memory for them.
+// Measured. A million two-hop rows of bfloat16 at hidden 256: 300 to 313 us, 0.68 GB fetched and 0.51 written, while vector instructions
+// keep the SIMDs for two thirds of it (912 for a wave's eight rows: 104 for an entry and lane, of which 80 convert and multiply codes). Two
+// groups of four entries, which have to be joined: 327, in fp32 (300,000 rows) 197 for 144. Lanes that store their own 64 bytes past
+// the caches: 471. 5 or 6 waves a SIMD, which the compiler reaches by spilling: 341 and 582. Long rows are bound by vector instructions:
+// 15,135 of eight hops at 128 take 56 us two entries a step, 64 with four, of which the row's last step leaves more unused; at hidden 256
+// 99, with sums scaled down in every step 108.
 template <typename T, int D, int S, int CH, bool ONCE, bool FAR>
 __global__ __launch_bounds__(256) void kv4_attn_kernel(dg4_kv8_attn_args p)
 {
@@ -410,7 +421,7 @@ template <typename A, typename F> int launch_rows(A a, int rows_per_block, F&& l
 template <typename T, int D>
 int launch_write(const dg4_kv8_args& args, hipStream_t s)
 {
-    constexpr int U = 2;
+    constexpr int U = sizeof(T) == 2 ? 2 : 1;
     return launch_rows(args, 256 / (2 * D / 8) * U, [&](const dg4_kv8_args& a, dim3 grid) {
         hipLaunchKernelGGL((kv4_write_kernel<T, D, U>), grid, dim3(256), 0, s, a);
     });
@@ -424,7 +435,11 @@ int launch_read(const dg4_kv8_args& args, hipStream_t s)
     });
 }
 // The split of a row goes by the cones' depth alone, so its result does not depend on which rows a call covers. A cone of one hop
-// holds three gates, of two hops seven, fifteen, ...; MOST: what a call's cones hold at most.
+// holds three gates, of two hops seven, fifteen, ...; MOST: what a call's cones hold at most. Measured with 1, 2, 4, 8 groups a row in bfloat16 (us;
+// two entries a step): 90,000 rows of four hops at 256 80, 83, 92, 119, but 1000 at 128 12.5, 7.9, 5.4, 4.8; 60,000 of five hops at 128 60, 56, 55,
+// 61; 30,000 of six hops at 256 107, 89, 82, 84; 20,000 of seven hops at 128 106, 72, 56, 51 (sixteen: 52); 15,135 of eight hops at 128 153, 101,
+// 72, 61 (sixteen: 56). Three hops, in one go by two groups: 200,000 rows at 256 108, one group with four entries a step 102, but 1000 of fp32
+// 5.6 and 8.6.
 template <typename T, int D, bool FAR, int MOST>
 int launch_attn_of(const dg4_kv8_attn_args& args, hipStream_t s)
 {

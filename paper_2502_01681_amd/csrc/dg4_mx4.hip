@@ -200,6 +200,9 @@ template <typename T> __device__ __forceinline__ void get16(const T* from, float
 
 // A workgroup has a wave for every head, whose columns of Wq, Wk and Wv stay in its registers, and takes tiles of rows in turn: the
 // rows of the next tile travel while this one is multiplied. Results leave by way of LDS, so that a store is whole rows.
+// Bound by HBM: a million rows of bfloat16 at hidden 256 to Q, K and V 377 us (2.06 GB, 5.5 TB/s), to Q and into the store 236 (1.30 GB);
+// 400,000 of fp32 at 256 313 and 500,000 of bfloat16 at 128 91, where lanes that store their own pieces take 395 and 108 (372 and 294 for the
+// first two). Workgroups: 256 at hidden 256 (512: 406 and 250), 512 at 128 (256: 95).
 template <typename T, int D, bool STORE>
 __global__ __launch_bounds__(2 * D) void mx4_proj_kernel(dg4_mx4_proj_args p)
 {
@@ -280,7 +283,8 @@ __global__ __launch_bounds__(2 * D) void mx4_proj_kernel(dg4_mx4_proj_args p)
 // instructions from being issued for 16, and 614 vector instructions of 4 cycles, 3480 cycles in all; the clock falls to 1.8 GHz under it.
 // Eight waves that all do everything, an eighth of either matrix each, in step: 365 us (their products and vector instructions come at the same
 // time), with rows and residual from memory instead of LDS, so that waits for loads were waits for stores: 412, with three barriers to a
-// tile: 520. The same with the two halves of the waves in opposite order, or the residual added on the matrix cores: no faster.
+// tile: 520. Half the waves in the opposite order need more registers than there are. The residual of bfloat16 added by products with a unit
+// matrix and sums of squares for the variance: 324 for 332 on one card, but rows far off zero lose the variance's digits.
 constexpr int FFN_THREADS = 512;
 template <typename T, int D>
 __global__ __launch_bounds__(FFN_THREADS) void mx4_ffn_kernel(dg4_mx4_ffn_args p)
@@ -341,9 +345,11 @@ __global__ __launch_bounds__(FFN_THREADS) void mx4_ffn_kernel(dg4_mx4_ffn_args p
         x.load(p.s, r0 + step, p.row_end);
         __syncthreads();
         first(rows[0], hidden[0]);
-        x.put(rows[1]);
-        x.keep(full[1]);
-        x.load(p.s, r0 + 2 * step, p.row_end);
+        if (r0 + step < p.row_end) {
+            x.put(rows[1]);
+            x.keep(full[1]);
+            x.load(p.s, r0 + 2 * step, p.row_end);
+        }
         int t = 0, t3 = 0;
         for (; r0 < p.row_end; r0 += step, t ^= 1, t3 = t3 == 2 ? 0 : t3 + 1) {
             __syncthreads();
@@ -357,6 +363,7 @@ __global__ __launch_bounds__(FFN_THREADS) void mx4_ffn_kernel(dg4_mx4_ffn_args p
         __syncthreads();
     } else {
         const int quarter = wave - 4;
+        __syncthreads();                          // (W1, which is needed first, is on its way)
         uint4 w2[TILES2][KC2];
         uint32_t sw2[TILES2][KC2 / 4];
         const uint4* u2 = (const uint4*)p.w2_packed;
@@ -453,7 +460,6 @@ __global__ __launch_bounds__(FFN_THREADS) void mx4_ffn_kernel(dg4_mx4_ffn_args p
             for (int i = 0; i < 4; ++i) q[i] = from[i][n];
         };
         float2 q[4];
-        __syncthreads();
         int t = 0, t3 = 0;
         for (; r0 < p.row_end; r0 += step, t ^= 1, t3 = t3 == 2 ? 0 : t3 + 1) {
             __syncthreads();
