@@ -348,8 +348,8 @@ __global__ __launch_bounds__(FFN_THREADS) void mx4_ffn_kernel(dg4_mx4_ffn_args p
         if (r0 + step < p.row_end) {
             x.put(rows[1]);
             x.keep(full[1]);
-            x.load(p.s, r0 + 2 * step, p.row_end);
         }
+        x.load(p.s, r0 + 2 * step, p.row_end);
         int t = 0, t3 = 0;
         for (; r0 < p.row_end; r0 += step, t ^= 1, t3 = t3 == 2 ? 0 : t3 + 1) {
             __syncthreads();
