@@ -215,10 +215,11 @@ template <> struct HeadQ<bf16_t> {
 // whole row at one go. Entries that are none (padding, a relation whose bias is -inf) ask the buffers for an offset past the end: zeros, no
 // request, no branch, and what the store holds there cannot matter. The offsets of buffer addressing are 32 bits: FAR, for larger stores,
 // has addresses of 64 bits and reads zeros from memory for them.
-// Measured. A million two-hop rows of bfloat16 at hidden 256: 300 to 313 us, 0.68 GB fetched and 0.51 written, while vector instructions
-// keep the SIMDs for two thirds of it (912 for a wave's eight rows: 104 for an entry and lane, of which 80 convert and multiply codes). Two
-// groups of four entries, which have to be joined: 327, in fp32 (300,000 rows) 197 for 144. Lanes that store their own 64 bytes past
-// the caches: 471. 5 or 6 waves a SIMD, which the compiler reaches by spilling: 341 and 582. Long rows are bound by vector instructions:
+// Measured. A million two-hop rows of bfloat16 at hidden 256, one source in five anywhere in the store: 300 to 313 us on several cards,
+// 1.36 GB fetched past the L2s and 0.51 written, 6.0 TB/s; vector instructions keep the SIMDs for two thirds of it (912 for a
+// wave's eight rows: 104 for an entry and lane, of which 80 convert and multiply codes). Six waves a SIMD instead of four (without the
+// branch for rows of Q that are odd) change nothing. Two groups of four entries, which have to be joined: 327, in fp32 (300,000 rows) 197
+// for 144. Lanes that store their own 64 bytes past the caches: 471; Q read past them: 366. Long rows are bound by vector instructions:
 // 15,135 of eight hops at 128 take 56 us two entries a step, 64 with four, of which the row's last step leaves more unused; at hidden 256
 // 99, with sums scaled down in every step 108.
 template <typename T, int D, int S, int CH, bool ONCE, bool FAR>
