@@ -540,7 +540,7 @@ def dg4_kv4_read(cfg: LayerConfig, codes, scales, K, V, ids=None, row_begin=0, r
 
 def dg4_sparse_attn_kv4_fwd(cfg: LayerConfig, g: Graph, Q, codes, scales, rel_bias, A, ids=None, row_begin=0, row_end=None):
     """Cone attention over the store in 4 bits (row = node id). ids: int32 gate of each row of Q and A, else the row itself."""
-    (_marshal_module or _marshal()).sparse_attn_kv4_fwd(cfg, g._h.value, g.n, Q, codes, scales, rel_bias, A, ids, row_begin, row_end)
+    (_marshal_module or _marshal()).sparse_attn_kv4_fwd(cfg, g._h.value if g._h else 0, g.n, Q, codes, scales, rel_bias, A, ids, row_begin, row_end)
 
 
 @dataclass

@@ -45,6 +45,12 @@ int64_t integer(PyObject* o)
     return v;
 }
 int64_t integer_of(PyObject* o, PyObject* name) { return integer(Ref(PyObject_GetAttr(o, name)).p); }
+int32_t small_of(PyObject* o, PyObject* name)
+{
+    const int64_t v = integer_of(o, name);
+    if (v != (int32_t)v) throw Refused{};
+    return (int32_t)v;
+}
 
 const at::Tensor& tensor(PyObject* o)
 {
@@ -60,9 +66,9 @@ struct Call {
     void* stream;
     Call(PyObject* c, const at::Tensor& first)
     {
-        cfg.hidden = (int32_t)integer_of(c, n_hidden);
-        cfg.heads = (int32_t)integer_of(c, n_heads);
-        cfg.hops = (int32_t)integer_of(c, n_hops);
+        cfg.hidden = small_of(c, n_hidden);
+        cfg.heads = small_of(c, n_heads);
+        cfg.hops = small_of(c, n_hops);
         cfg.n_layers = 1;
         const Ref eps(PyObject_GetAttr(c, n_ln_eps));
         cfg.ln_eps = (float)PyFloat_AsDouble(eps.p);
@@ -124,16 +130,15 @@ struct Store {
 
 // Weights [k, n] of dg4_mx4_pack
 struct Packed {
+    Ref packed;
     void* at;
     int64_t bytes;
-    Packed(const Call& c, PyObject* w, int64_t k, int64_t n)
+    Packed(const Call& c, PyObject* w, int64_t k, int64_t n) : packed(PyObject_GetAttr(w, n_packed))
     {
         if (integer_of(w, n_hidden) != c.cfg.hidden || integer_of(w, n_k) != k || integer_of(w, n_n) != n) throw Refused{};
-        const Ref packed(PyObject_GetAttr(w, n_packed));
         const at::Tensor& t = tensor(packed.p);
-        if (t.get_device() != c.dev) throw Refused{};
-        at = t.data_ptr();
         bytes = t.numel();
+        at = c.at(t, at::kByte, bytes);
     }
 };
 

@@ -395,6 +395,44 @@ def test_more_rows_than_a_launch_holds():
     assert torch.equal(A, A[1:2].expand_as(A))
 
 
+@pytest.mark.parametrize("hidden,dtype", SHAPES)
+@pytest.mark.parametrize("how,hops", [("device", 2), ("device", 6), ("partitioned", 2), ("partitioned", 3), ("partitioned", 8), ("copies", 2), ("copies", 5)])
+def test_attention_over_other_graphs(hidden, dtype, how, hops):
+    """Rows of graphs that the device analysed, rows that a partition restricts, rows of its copies of gates."""
+    n = 260
+    rng = np.random.default_rng(hops)
+    src, dst, inv = [], [], []
+    for v in range(12, n):
+        a, b = rng.choice(np.arange(max(0, v - 40), v), 2, replace=False)
+        for u in ([a] if rng.random() < 0.1 else [a, b]):
+            src.append(u); dst.append(v); inv.append(int(rng.random() < 0.4))
+    if how == "device":
+        up = lambda x, t: torch.tensor(x, dtype=t, device="cuda")
+        g = dg4.dg4_build_levels_device(n, up(src, torch.int32), up(dst, torch.int32), up(inv, torch.uint8), hops)
+    else:
+        g = dg4.dg4_build_partitioned(n, src, dst, inv, hops, hops - 1, 16, marks=how == "partitioned")
+    print(f"kv4 attention, {how}, {hidden} {dtype} hops={hops} rows={g.n}", flush=True)
+    codes, scales = store(5, g.n, hidden)
+    Q = torch.from_numpy(rng.standard_normal((g.n, hidden)).astype(np.float32)).to(tdtype(dtype)).cuda()
+    bias = torch.from_numpy(rng.standard_normal((hidden // 32, 4)).astype(np.float32)).cuda()
+    A = attend(cfg(hidden, dtype, hops), g, Q, codes, scales, bias)
+    close(A, *reference(g, range(g.n), Q, codes, scales, bias, dtype))
+
+
+def test_a_graph_that_is_closed_and_a_configuration_past_32_bits():
+    n, hidden = 4, 128
+    x, (codes, scales), bias = torch.zeros((n, hidden), device="cuda"), blank(n, hidden), torch.zeros((4, 4), device="cuda")
+    g = dg4.dg4_build_levels(n, [0, 1], [2, 2], [0, 1], 2)
+    dg4.dg4_sparse_attn_kv4_fwd(cfg(hidden, "f32"), g, x, codes, scales, bias, x)
+    far = [dg4.LayerConfig(2 ** 32 + hidden, 4, 2, 1, "f32"), dg4.LayerConfig(hidden, 2 ** 32 + 4, 2, 1, "f32"), dg4.LayerConfig(hidden, 4, 2 ** 32 + 2, 1, "f32")]
+    for c in far:
+        with pytest.raises(dg4.DG4Error):
+            dg4.dg4_sparse_attn_kv4_fwd(c, g, x, codes, scales, bias, x)
+    g.close()
+    with pytest.raises(dg4.DG4Error):
+        dg4.dg4_sparse_attn_kv4_fwd(cfg(hidden, "f32"), g, x, codes, scales, bias, x)
+
+
 def test_binding_checks():
     """Shapes, types and places that do not fit are turned away before anything is queued; nothing to do is fine."""
     n, hidden = 6, 128

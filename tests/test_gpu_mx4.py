@@ -277,6 +277,37 @@ def test_two_threads_share_weights():
     assert not failed and all(torch.equal(a, b) for x, y in zip(got, want) for a, b in zip(x, y))
 
 
+@pytest.mark.parametrize("hidden,dtype", SHAPES)
+@pytest.mark.parametrize("rows", [8160, 8192, 8193, 16385, 24576, 24609, 33000])
+def test_rows_around_what_workgroups_take_at_once(hidden, dtype, rows):
+    """One tile, two, three and four to a workgroup, whole and not, against calls of few rows (a row's result depends on nothing else)."""
+    print(f"mx4 {rows} rows of {hidden} {dtype}", flush=True)
+    c = cfg(hidden, dtype)
+    S = torch.empty((rows, hidden), dtype=tdtype(dtype), device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(rows))
+    packed, w1, w2 = (dg4.dg4_mx4_pack(c, matrix(i, k, m, dtype)) for i, (k, m) in enumerate(((hidden, 3 * hidden), (hidden, 4 * hidden), (4 * hidden, hidden))))
+    whole, parts = [*project(c, packed, S), feed(c, w1, w2, S)], [torch.empty_like(S) for _ in range(4)]
+    store = blank(rows, hidden), blank(rows, hidden)
+    Q = torch.empty_like(S)
+    dg4.dg4_qkv_proj_kv4(c, packed, S, Q, *store[0])
+    assert torch.equal(Q, whole[0])
+    for lo in range(0, rows, 3000):
+        kw = dict(row_begin=lo, row_end=min(rows, lo + 3000))
+        dg4.dg4_qkv_proj_mx4(c, packed, S, *parts[:3], **kw)
+        dg4.dg4_ffn_mx4_fwd(c, w1, w2, S, parts[3], **kw)
+        dg4.dg4_qkv_proj_kv4(c, packed, S, Q, *store[1], **kw)
+    assert all(torch.equal(a, b) for a, b in zip(whole, parts)) and torch.equal(Q, whole[0])
+    assert all(torch.equal(a, b) for a, b in zip(*store))
+
+
+def test_packed_weights_that_are_not_whole_are_refused():
+    c = cfg(128, "f32")
+    w = dg4.dg4_mx4_pack(c, torch.zeros((128, 384), device="cuda"))
+    x = [torch.zeros((3, 128), device="cuda") for _ in range(4)]
+    for packed in (w.packed[:1].expand(w.packed.numel()), w.packed.view(torch.int32), w.packed[:-256], w.packed[16:], w.packed.cpu()):
+        with pytest.raises(dg4.DG4Error):
+            dg4.dg4_qkv_proj_mx4(c, dg4.Mx4Weights(packed, 128, 384, 128), *x)
+
+
 @pytest.mark.parametrize("hidden,dtype", [(256, "bf16"), (128, "f32")])
 def test_rows_past_four_gigabytes(hidden, dtype):
     """Rows on both sides of every mark of 4.4 GB arrays against calls of those rows alone (a row's result depends on nothing else)."""
