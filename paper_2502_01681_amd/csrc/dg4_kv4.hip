@@ -408,14 +408,13 @@ __global__ __launch_bounds__(256) void kv4_attn_kernel(dg4_kv8_attn_args p)
     }
 }
 
-// launch(args, workgroups) for the rows of a call. A launch holds fewer than 2^32 threads, 2^24 workgroups: longer calls take several.
-template <typename A, typename F> int launch_rows(A a, int rows_per_block, F&& launch)
+// f(args, workgroups), a launch, for the rows of a call. A launch holds fewer than 2^32 threads, 2^24 workgroups: longer calls take several.
+template <typename A, typename F> int launch_rows(A a, int rows_per_block, F&& f)
 {
     const int64_t end = a.row_end, most = ((int64_t)1 << 23) * rows_per_block;
     for (; a.row_begin < end; a.row_begin = a.row_end) {
         a.row_end = std::min(end, a.row_begin + most);
-        launch(a, dim3((unsigned)((a.row_end - a.row_begin + rows_per_block - 1) / rows_per_block)));
-        if (const int e = hipGetLastError(); e != hipSuccess) return e;
+        if (const int e = f(a, dim3((unsigned)((a.row_end - a.row_begin + rows_per_block - 1) / rows_per_block))); e != hipSuccess) return e;
     }
     return hipSuccess;
 }
@@ -424,7 +423,7 @@ int launch_write(const dg4_kv8_args& args, hipStream_t s)
 {
     constexpr int U = sizeof(T) == 2 ? 2 : 1;
     return launch_rows(args, 256 / (2 * D / 8) * U, [&](const dg4_kv8_args& a, dim3 grid) {
-        hipLaunchKernelGGL((kv4_write_kernel<T, D, U>), grid, dim3(256), 0, s, a);
+        return launch(kv4_write_kernel<T, D, U>, grid, 256, s, a);
     });
 }
 template <typename T, int D>
@@ -432,7 +431,7 @@ int launch_read(const dg4_kv8_args& args, hipStream_t s)
 {
     constexpr int U = 2;
     return launch_rows(args, 256 / (2 * D / (16 / (int)sizeof(T))) * U, [&](const dg4_kv8_args& a, dim3 grid) {
-        hipLaunchKernelGGL((kv4_read_kernel<T, D, U>), grid, dim3(256), 0, s, a);
+        return launch(kv4_read_kernel<T, D, U>, grid, 256, s, a);
     });
 }
 // The split of a row goes by the cones' depth alone, so its result does not depend on which rows a call covers. A cone of one hop
@@ -449,7 +448,7 @@ int launch_attn_of(const dg4_kv8_attn_args& args, hipStream_t s)
     constexpr int S = MOST <= 7 ? 1 : MOST <= 31 ? 2 : MOST <= 127 ? 4 : MOST <= 255 ? 8 : GPW;
     constexpr int CH = MOST <= 7 ? MOST : ONCE ? 8 : 2;
     return launch_rows(args, 4 * GPW / S, [&](const dg4_kv8_attn_args& a, dim3 grid) {
-        hipLaunchKernelGGL((kv4_attn_kernel<T, D, S, CH, ONCE, FAR>), grid, dim3(256), 0, s, a);
+        return launch(kv4_attn_kernel<T, D, S, CH, ONCE, FAR>, grid, 256, s, a);
     });
 }
 template <typename T, int D, bool FAR>

@@ -493,9 +493,7 @@ int64_t dg4_mx4_bytes(int k, int n)
 int dg4_launch_mx4_pack(int dtype, const dg4_mx4_pack_args& a, hipStream_t s)
 {
     const dim3 grid((unsigned)((a.k / 32 * a.n + 255) / 256));
-    if (dtype == DG4_F32) hipLaunchKernelGGL(mx4_pack_kernel<float>, grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL(mx4_pack_kernel<bf16_t>, grid, dim3(256), 0, s, a);
-    return hipGetLastError();
+    return launch(dtype == DG4_F32 ? mx4_pack_kernel<float> : mx4_pack_kernel<bf16_t>, grid, 256, s, a);
 }
 int dg4_launch_mx4_proj(int dtype, int hidden, const dg4_mx4_proj_args& a, hipStream_t s)
 {
@@ -503,9 +501,7 @@ int dg4_launch_mx4_proj(int dtype, int hidden, const dg4_mx4_proj_args& a, hipSt
         using T = decltype(t);
         constexpr int D = d.value;
         const dim3 grid = walks(a.row_end - a.row_begin, D == 256 ? 256 : 512);
-        if (a.codes) hipLaunchKernelGGL((mx4_proj_kernel<T, D, true>), grid, dim3(2 * D), 0, s, a);
-        else hipLaunchKernelGGL((mx4_proj_kernel<T, D, false>), grid, dim3(2 * D), 0, s, a);
-        return (int)hipGetLastError();
+        return launch(a.codes ? mx4_proj_kernel<T, D, true> : mx4_proj_kernel<T, D, false>, grid, 2 * D, s, a);
     });
 }
 int dg4_launch_mx4_ffn(int dtype, int hidden, const dg4_mx4_ffn_args& a, hipStream_t s)
@@ -513,7 +509,6 @@ int dg4_launch_mx4_ffn(int dtype, int hidden, const dg4_mx4_ffn_args& a, hipStre
     return by_shape(dtype, hidden, [&](auto t, auto d) {
         using T = decltype(t);
         constexpr int D = d.value;
-        hipLaunchKernelGGL((mx4_ffn_kernel<T, D>), walks(a.row_end - a.row_begin, D == 256 ? 256 : 512), dim3(FFN_THREADS), 0, s, a);
-        return (int)hipGetLastError();
+        return launch(mx4_ffn_kernel<T, D>, walks(a.row_end - a.row_begin, D == 256 ? 256 : 512), FFN_THREADS, s, a);
     });
 }
