@@ -438,8 +438,8 @@ int launch_read(const dg4_kv8_args& args, hipStream_t s)
 // holds three gates, of two hops seven, fifteen, ...; MOST: what a call's cones hold at most. Measured with 1, 2, 4, 8 groups a row in bfloat16 (us;
 // two entries a step): 90,000 rows of four hops at 256 80, 83, 92, 119, but 1000 at 128 12.5, 7.9, 5.4, 4.8; 60,000 of five hops at 128 60, 56, 55,
 // 61; 30,000 of six hops at 256 107, 89, 82, 84; 20,000 of seven hops at 128 106, 72, 56, 51 (sixteen: 52); 15,135 of eight hops at 128 153, 101,
-// 72, 61 (sixteen: 56). Three hops, in one go by two groups: 200,000 rows at 256 108, one group with four entries a step 102, but 1000 of fp32
-// 5.6 and 8.6.
+// 72, 61 (sixteen: 56). Three hops, in one go by two groups: 200,000 rows at 256 101 (one group with four entries a step 102), 1000 of fp32 5.6
+// (8.6).
 template <typename T, int D, bool FAR, int MOST>
 int launch_attn_of(const dg4_kv8_attn_args& args, hipStream_t s)
 {
