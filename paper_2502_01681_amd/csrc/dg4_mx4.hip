@@ -72,8 +72,9 @@ template <int N, int C = 0, typename F> __device__ __forceinline__ void each(F&&
     }
 }
 
-// Rows in 4 bits in LDS, as B operand: 16 bytes of codes per block, a word of scale bytes for every four chunks and parity of the block
-template <int D> struct MxRows {
+// What stands in LDS goes in and out in pieces of 16 bytes, so every row of it is whole pieces at a whole piece's address.
+// Rows in 4 bits, as B operand: 16 bytes of codes per block, a word of scale bytes for every four chunks and parity of the block
+template <int D> struct alignas(16) MxRows {
     static constexpr int STRIDE = D / 2 + 16;     // bytes
     static constexpr int WORDS = (D / 32 + 7) / 8 * 2;         // scale words of a row
     uint8_t codes[ROWS][STRIDE];
@@ -86,8 +87,14 @@ template <int D> struct MxRows {
     __device__ __forceinline__ uint32_t scale(int n, int hi, int c) const { return scales[c / 4 * 2 + hi][n]; }
 };
 
-// Rows as they are, in LDS
-template <typename T, int D> struct FullRows { T x[ROWS][D + 16 / (int)sizeof(T)]; };
+// Rows as they are
+template <typename T, int D> struct alignas(16) FullRows { T x[ROWS][D + 16 / (int)sizeof(T)]; };
+
+// Rows of the store, K | V codes and scale bytes
+template <int D> struct alignas(16) StoreRows {
+    uint8_t codes[ROWS][D + 16];
+    uint8_t scales[ROWS][2 * D / 32];             // (in pieces of 8)
+};
 
 // Rows of a tile as a buffer: what lies behind the call's last row reads as zeros and is not written, without a branch (behind
 // which a wait for loads would be one for every store before it, too). No rows at all (r0 past the end, or not yet there): nothing.
@@ -209,7 +216,8 @@ __global__ __launch_bounds__(2 * D) void mx4_proj_kernel(dg4_mx4_proj_args p)
     constexpr int HEADS = D / 32, KC = D / 64, OUTS = STORE ? 1 : 3;
     __shared__ MxRows<D> rows[2];
     __shared__ FullRows<T, D> outs[OUTS];
-    __shared__ uint8_t codes[STORE ? ROWS : 1][D + 16], scales[STORE ? ROWS : 1][2 * HEADS];
+    struct Nothing {};
+    __shared__ std::conditional_t<STORE, StoreRows<D>, Nothing> kv;
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 31, hi = lane >> 5;
@@ -243,8 +251,8 @@ __global__ __launch_bounds__(2 * D) void mx4_proj_kernel(dg4_mx4_proj_args p)
             if constexpr (STORE) {
                 if (j > 0) {
                     const uint32_t byte = fp4_scale_byte(block_top<false>(acc));
-                    *(uint2*)(codes[n] + (j - 1) * (D / 2) + wave * 16 + hi * 8) = byte == FP4_BAD ? make_uint2(0, 0) : half_codes(acc, byte << 23);
-                    scales[n][wave * 2 + j - 1] = (uint8_t)byte;               // (lane ^ 32 the same)
+                    *(uint2*)(kv.codes[n] + (j - 1) * (D / 2) + wave * 16 + hi * 8) = byte == FP4_BAD ? make_uint2(0, 0) : half_codes(acc, byte << 23);
+                    kv.scales[n][wave * 2 + j - 1] = (uint8_t)byte;               // (lane ^ 32 the same)
                     continue;
                 }
             }
@@ -267,8 +275,8 @@ __global__ __launch_bounds__(2 * D) void mx4_proj_kernel(dg4_mx4_proj_args p)
             int64_t at = -1;
             if (r < p.row_end) at = p.ids ? (int64_t)p.ids[r] : r;
             if (at >= 0 && at < p.n_store) {
-                *(uint4*)(p.codes + at * D + piece * 16) = *(const uint4*)(codes[row] + piece * 16);
-                if (piece < HEADS / 4) *(uint2*)(p.scales + at * (2 * HEADS) + piece * 8) = *(const uint2*)(scales[row] + piece * 8);
+                *(uint4*)(p.codes + at * D + piece * 16) = *(const uint4*)(kv.codes[row] + piece * 16);
+                if (piece < HEADS / 4) *(uint2*)(p.scales + at * (2 * HEADS) + piece * 8) = *(const uint2*)(kv.scales[row] + piece * 8);
             }
         }
     }
