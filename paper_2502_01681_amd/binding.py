@@ -515,10 +515,11 @@ def _marshal():
         import importlib.machinery
         import importlib.util
         import torch
-        if not os.path.exists(_build.MARSHAL):
+        path = os.path.join(_build.HERE, _build.MARSHAL)
+        if not os.path.exists(path):
             _build.build(force=False)
-        loader = importlib.machinery.ExtensionFileLoader("_dg4_marshal", _build.MARSHAL)
-        m = importlib.util.module_from_spec(importlib.util.spec_from_file_location("_dg4_marshal", _build.MARSHAL, loader=loader))
+        loader = importlib.machinery.ExtensionFileLoader("_dg4_marshal", path)
+        m = importlib.util.module_from_spec(importlib.util.spec_from_file_location("_dg4_marshal", path, loader=loader))
         loader.exec_module(m)
         names = ("dg4_kv4_write", "dg4_kv4_read", "dg4_sparse_attn_kv4_fwd", "dg4_qkv_proj_mx4", "dg4_qkv_proj_kv4", "dg4_ffn_mx4_fwd")
         m.bind(*(ctypes.cast(getattr(lib(), n), _P).value for n in names), DG4Error, torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice)

@@ -1,4 +1,4 @@
-"""Build libdg4.so (HIP kernels + C ABI) in-tree for gfx950, and the native part of the Python binding."""
+"""Build libdg4.so (HIP kernels + C ABI) in-tree for gfx950 and, where torch is installed, the native part of the Python binding."""
 from __future__ import annotations
 
 import importlib.util
@@ -11,7 +11,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdg4.so")
-MARSHAL = os.path.join(HERE, "_dg4_marshal.so")
+MARSHAL = "_dg4_marshal.so"
 OBJ = os.path.join(HERE, "_build")
 SOURCES = ["dg4_graph.cpp", "dg4_graph_gpu.hip", "dg4_api.cpp", "dg4_kernels.hip", "dg4_sweep.hip", "dg4_flow.hip", "dg4_heads.hip",
            "dg4_static.hip", "dg4_kv8.hip", "dg4_lora.hip", "dg4_kv4.hip", "dg4_mx4.hip"]
@@ -24,11 +24,22 @@ def sources():
     return [os.path.join(CSRC, s) for s in SOURCES]
 
 
+def _torch():
+    """Folder of torch, None without it (which is not imported)."""
+    spec = importlib.util.find_spec("torch")
+    return spec and os.path.dirname(spec.origin)
+
+
+def _older(path, sources) -> bool:
+    return not os.path.exists(path) or any(os.path.getmtime(d) > os.path.getmtime(path) for d in sources)
+
+
+def _stale_marshal() -> bool:
+    return _torch() is not None and _older(os.path.join(HERE, MARSHAL), [MARSHAL_SOURCE] + HEADERS)
+
+
 def stale() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(MARSHAL):
-        return True
-    t = min(os.path.getmtime(LIB), os.path.getmtime(MARSHAL))
-    return any(os.path.getmtime(d) > t for d in sources() + HEADERS + [MARSHAL_SOURCE])
+    return _older(LIB, sources() + HEADERS) or _stale_marshal()
 
 
 def _flags():
@@ -47,15 +58,16 @@ def _flags():
 
 def _build_marshal():
     """The native part of the Python binding (host code, against this interpreter and torch)."""
-    torch = os.path.dirname(importlib.util.find_spec("torch").origin)
+    torch = _torch()
     subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-I", sysconfig.get_paths()["include"],
-                           "-isystem", os.path.join(torch, "include"), "-I", os.path.join(ROOT, "include"), MARSHAL_SOURCE, "-o", MARSHAL,
+                           "-isystem", os.path.join(torch, "include"), "-I", os.path.join(ROOT, "include"), MARSHAL_SOURCE, "-o", os.path.join(HERE, MARSHAL),
                            "-L", os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"])
 
 
 def build(force: bool = True) -> str:
     """Compile every source with hipcc for gfx950 (one object per source, in parallel) and link the
-    shared library. force=False recompiles only the sources that changed since their object was made."""
+    shared library, whether or not the module beside it can be built. force=False recompiles only the sources
+    that changed since their object was made."""
     if not force and not stale():
         return LIB
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -70,11 +82,11 @@ def build(force: bool = True) -> str:
         return obj
 
     with ThreadPoolExecutor(max_workers=min(8, len(SOURCES))) as ex:
-        marshal = ex.submit(_build_marshal) if force or not os.path.exists(MARSHAL) or os.path.getmtime(MARSHAL) < max(os.path.getmtime(MARSHAL_SOURCE), newest_header) else None
+        marshal = ex.submit(_build_marshal) if _stale_marshal() or force and _torch() else None
         objs = list(ex.map(compile_one, sources()))
+        subprocess.check_call([hipcc, "-shared", "-fPIC", "--offload-arch=gfx950", "-o", LIB] + objs)
         if marshal is not None:
             marshal.result()
-    subprocess.check_call([hipcc, "-shared", "-fPIC", "--offload-arch=gfx950", "-o", LIB] + objs)
     return LIB
 
 
