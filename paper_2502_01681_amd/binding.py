@@ -86,9 +86,7 @@ def lib():
     """The loaded C library. Built first if absent; a failure to load is fatal by design."""
     global _lib
     if _lib is None:
-        if not os.path.exists(_build.LIB):
-            _build.build()
-        L = ctypes.CDLL(_build.LIB)
+        L = ctypes.CDLL(_build.library())
         L.dg4_strerror.restype = ctypes.c_char_p
         L.dg4_strerror.argtypes = [ctypes.c_int]
         L.dg4_build_levels.restype = ctypes.c_int
@@ -515,9 +513,7 @@ def _marshal():
         import importlib.machinery
         import importlib.util
         import torch
-        path = os.path.join(_build.HERE, _build.MARSHAL)
-        if not os.path.exists(path):
-            _build.build(force=False)
+        path = _build.marshal()
         loader = importlib.machinery.ExtensionFileLoader("_dg4_marshal", path)
         m = importlib.util.module_from_spec(importlib.util.spec_from_file_location("_dg4_marshal", path, loader=loader))
         loader.exec_module(m)

@@ -1,6 +1,10 @@
 """Build libdg4.so (HIP kernels + C ABI) in-tree for gfx950 and, where torch is installed, the native part of the Python binding."""
 from __future__ import annotations
 
+import contextlib
+import fcntl
+import glob
+import hashlib
 import importlib.util
 import os
 import subprocess
@@ -11,13 +15,13 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdg4.so")
-MARSHAL = "_dg4_marshal.so"
 OBJ = os.path.join(HERE, "_build")
 SOURCES = ["dg4_graph.cpp", "dg4_graph_gpu.hip", "dg4_api.cpp", "dg4_kernels.hip", "dg4_sweep.hip", "dg4_flow.hip", "dg4_heads.hip",
            "dg4_static.hip", "dg4_kv8.hip", "dg4_lora.hip", "dg4_kv4.hip", "dg4_mx4.hip"]
 HEADERS = [os.path.join(CSRC, h) for h in ("dg4_internal.h", "dg4_device.h", "dg4_rowops.h", "dg4_wait.h", "dg4_fp4.h")] + [os.path.join(ROOT, "include", h) for h in ("dg4.h", "dg4_serving.h", "dg4_mx4.h")]
 
 MARSHAL_SOURCE = os.path.join(CSRC, "dg4_marshal.cpp")
+MARSHAL_HEADERS = [os.path.join(ROOT, "include", h) for h in ("dg4.h", "dg4_serving.h", "dg4_mx4.h")]
 
 
 def sources():
@@ -34,12 +38,34 @@ def _older(path, sources) -> bool:
     return not os.path.exists(path) or any(os.path.getmtime(d) > os.path.getmtime(path) for d in sources)
 
 
-def _stale_marshal() -> bool:
-    return _torch() is not None and _older(os.path.join(HERE, MARSHAL), [MARSHAL_SOURCE] + HEADERS)
+def _marshal_path() -> str:
+    """Where the native part of the binding stands: by the interpreter, torch and sources that it is built from, so that a module of
+    others is not taken for it."""
+    digest = hashlib.sha256()
+    for path in [os.path.join(_torch(), "version.py"), MARSHAL_SOURCE] + MARSHAL_HEADERS:
+        with open(path, "rb") as f:
+            digest.update(f.read())
+    return os.path.join(HERE, "_dg4_marshal-" + digest.hexdigest()[:12] + sysconfig.get_config_var("EXT_SUFFIX"))
 
 
 def stale() -> bool:
-    return _older(LIB, sources() + HEADERS) or _stale_marshal()
+    return _older(LIB, sources() + HEADERS) or _torch() is not None and not os.path.exists(_marshal_path())
+
+
+@contextlib.contextmanager
+def _alone():
+    """One at a time builds, among threads and processes."""
+    os.makedirs(OBJ, exist_ok=True)
+    with open(os.path.join(OBJ, "lock"), "w") as f:
+        fcntl.flock(f, fcntl.LOCK_EX)
+        yield
+
+
+def _write(path, command):
+    """command, a link of which -o is `path`: what stands there is whole at any time, and mapped files are not written to."""
+    new = os.path.join(OBJ, os.path.basename(path))
+    subprocess.check_call(command + ["-o", new])
+    os.replace(new, path)
 
 
 def _flags():
@@ -56,22 +82,43 @@ def _flags():
             "-Wall", "-Wno-unused-function"]
 
 
-def _build_marshal():
+def _build_marshal(path):
     """The native part of the Python binding (host code, against this interpreter and torch)."""
     torch = _torch()
-    subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-I", sysconfig.get_paths()["include"],
-                           "-isystem", os.path.join(torch, "include"), "-I", os.path.join(ROOT, "include"), MARSHAL_SOURCE, "-o", os.path.join(HERE, MARSHAL),
-                           "-L", os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"])
+    _write(path, [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-I", sysconfig.get_paths()["include"],
+                  "-isystem", os.path.join(torch, "include"), "-I", os.path.join(ROOT, "include"), MARSHAL_SOURCE,
+                  "-L", os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"])
+
+
+def library() -> str:
+    """Path of the shared library, built first if it is not there."""
+    if not os.path.exists(LIB):
+        with _alone():
+            if not os.path.exists(LIB):
+                _build(force=True)
+    return LIB
+
+
+def marshal() -> str:
+    """Path of the native part of the binding, built first if it is not there."""
+    path = _marshal_path()
+    if not os.path.exists(path):
+        with _alone():
+            if not os.path.exists(path):
+                _build_marshal(path)
+    return path
 
 
 def build(force: bool = True) -> str:
     """Compile every source with hipcc for gfx950 (one object per source, in parallel) and link the
     shared library, whether or not the module beside it can be built. force=False recompiles only the sources
     that changed since their object was made."""
-    if not force and not stale():
-        return LIB
+    with _alone():
+        return LIB if not force and not stale() else _build(force)
+
+
+def _build(force):
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    os.makedirs(OBJ, exist_ok=True)
     newest_header = max(os.path.getmtime(h) for h in HEADERS)
 
     def compile_one(src):
@@ -82,11 +129,15 @@ def build(force: bool = True) -> str:
         return obj
 
     with ThreadPoolExecutor(max_workers=min(8, len(SOURCES))) as ex:
-        marshal = ex.submit(_build_marshal) if _stale_marshal() or force and _torch() else None
+        path = _marshal_path() if _torch() else None
+        module = ex.submit(_build_marshal, path) if path and (force or not os.path.exists(path)) else None
         objs = list(ex.map(compile_one, sources()))
-        subprocess.check_call([hipcc, "-shared", "-fPIC", "--offload-arch=gfx950", "-o", LIB] + objs)
-        if marshal is not None:
-            marshal.result()
+        _write(LIB, [hipcc, "-shared", "-fPIC", "--offload-arch=gfx950"] + objs)
+        if module is not None:
+            module.result()
+            for other in glob.glob(os.path.join(HERE, "_dg4_marshal*.so")):    # of sources or a torch that are no more
+                if other != path:
+                    os.remove(other)
     return LIB
 
 

@@ -3,6 +3,9 @@ for by what writes files (no device)."""
 import importlib.util
 import os
 import subprocess
+import sys
+import sysconfig
+import time
 
 import pytest
 
@@ -54,3 +57,81 @@ def test_the_library_does_not_wait_for_a_module_that_cannot_be_built(elsewhere, 
     with pytest.raises(subprocess.CalledProcessError):
         build.build()
     assert os.path.exists(build.LIB) and len(linked(elsewhere)) == 1
+
+
+COMPILER = """#!{python}
+import os, sys, time
+to = sys.argv[sys.argv.index("-o") + 1]
+with open({log!r}, "a") as f:
+    f.write(to + "\\n")
+with open(to, "wb", buffering=0) as f:
+    f.write(b"x" * 1000)
+    time.sleep(1.0)
+    f.write(b"y" * 1000)
+"""
+
+FIRST_USE = """
+import sys, threading
+sys.path.insert(0, {root!r})
+from paper_2502_01681_amd import build
+build.HERE = {here!r}
+build.OBJ = {here!r} + "/_build"
+build.LIB = {here!r} + "/libdg4.so"
+build.SOURCES = build.SOURCES[:1]
+print("ready", flush=True)
+sys.stdin.readline()
+got = []
+def run():
+    path = build.{what}()
+    got.append(open(path, "rb").read() == b"x" * 1000 + b"y" * 1000)
+threads = [threading.Thread(target=run) for _ in range(3)]
+[t.start() for t in threads]
+[t.join() for t in threads]
+assert got == [True] * 3, got
+"""
+
+
+@pytest.mark.parametrize("what", ["marshal", "library"])
+def test_those_who_need_it_first_wait_for_one_build(tmp_path, what):
+    """Three threads in each of three processes, started while a slow compiler has written half of it: one build, and every one of
+    them reads it whole."""
+    log, compiler = tmp_path / "log", tmp_path / "compiler"
+    compiler.write_text(COMPILER.format(python=sys.executable, log=str(log)))
+    compiler.chmod(0o755)
+    env = dict(os.environ, CXX=str(compiler), HIPCC=str(compiler))
+    code = FIRST_USE.format(root=build.ROOT, here=str(tmp_path), what=what)
+    users = [subprocess.Popen([sys.executable, "-c", code], env=env, stdin=subprocess.PIPE, stdout=subprocess.PIPE, text=True) for _ in range(3)]
+    for u in users:
+        assert u.stdout.readline() == "ready\n"
+    for u in users:
+        u.stdin.write("go\n")
+        u.stdin.flush()
+        time.sleep(0.3)
+    for u in users:
+        u.communicate(timeout=60)
+        assert u.returncode == 0
+    written = [os.path.basename(x) for x in log.read_text().split()]
+    assert sorted(set(written)) == sorted(written), written
+
+
+def test_a_module_of_other_sources_or_another_torch_is_not_taken(tmp_path, monkeypatch):
+    here = build._marshal_path()
+    assert here == build._marshal_path() and here.endswith(sysconfig.get_config_var("EXT_SUFFIX"))
+    header = tmp_path / "dg4_mx4.h"
+    header.write_text("other")
+    with monkeypatch.context() as m:
+        m.setattr(build, "MARSHAL_HEADERS", build.MARSHAL_HEADERS[:-1] + [str(header)])
+        assert build._marshal_path() != here
+    (tmp_path / "version.py").write_text("__version__ = '0'")
+    with monkeypatch.context() as m:
+        m.setattr(build, "_torch", lambda: str(tmp_path))
+        assert build._marshal_path() != here
+
+
+def test_a_build_leaves_the_module_that_it_is_for(elsewhere):
+    old = os.path.join(build.HERE, "_dg4_marshal-of-old.so")
+    open(old, "w").close()
+    build.build()
+    assert os.listdir(build.HERE).count(os.path.basename(old)) == 0 and os.path.exists(build._marshal_path()) and len(modules(elsewhere)) == 1
+    build.build(force=False)
+    assert len(modules(elsewhere)) == 1
