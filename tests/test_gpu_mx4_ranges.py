@@ -1,0 +1,103 @@
+"""The calls in 4 bits at the ends of their ranges: calls of several launches."""
+import ctypes
+import re
+
+import numpy as np
+import pytest
+import torch
+
+import fp4_ref as ref
+import paper_2502_01681_amd as dg4
+from gpu_utils import tdtype, to_np
+
+pytestmark = pytest.mark.gpu
+
+def cfg(hidden, dtype, hops=2, **kw):
+    return dg4.LayerConfig(hidden, hidden // 32, hops, 1, dtype, **kw)
+
+
+def table(rng, shape, size, dtype):
+    """Normal numbers times size, rounded to the type, on the host."""
+    return torch.from_numpy((rng.standard_normal(shape).clip(-3.5, 3.5) * size).astype(np.float32)).to(tdtype(dtype))
+
+
+def launches(call):
+    """How many kernels a call launches: what a capture of it holds (nothing is run)."""
+    graph = torch.cuda.CUDAGraph(keep_graph=True)
+    with torch.cuda.graph(graph):
+        call()
+    path = re.search(r"\S*libamdhip64\.so\S*", open("/proc/self/maps").read()).group(0)
+    nodes = ctypes.c_size_t(0)
+    assert ctypes.CDLL(path).hipGraphGetNodes(ctypes.c_void_p(graph.raw_cuda_graph()), None, ctypes.byref(nodes)) == 0
+    return nodes.value
+
+
+def around(limit, rows):
+    return torch.tensor([0, 3, limit - 2, limit - 1, limit, limit + 1, limit + 3, rows - 1], device="cuda")
+
+
+def test_attention_in_several_launches():
+    """Rows of eight hops at hidden 128, four of them to a workgroup: 2^25 to a launch."""
+    hidden, n, limit = 128, 400, 2 ** 25
+    rows = limit + 5
+    c = cfg(hidden, "bf16", 8)
+    print(f"kv4 attention over {rows} rows, nearly all padding", flush=True)
+    rng = np.random.default_rng(1)
+    fan = [(u, v, int(rng.integers(0, 2))) for v in range(30, n) for u in rng.choice(np.arange(max(0, v - 40), v), 2, replace=False)]
+    g = dg4.dg4_build_levels(n, *(np.array(x) for x in zip(*fan)), 8)
+    g.upload()
+    codes = torch.zeros((n, hidden), dtype=torch.uint8, device="cuda")
+    scales = torch.zeros((n, hidden // 32, 2), dtype=torch.uint8, device="cuda")
+    dg4.dg4_kv4_write(c, *(table(rng, (n, hidden), 1.0, "bf16").cuda() for _ in range(2)), codes, scales)
+    bias = torch.zeros((hidden // 32, 4), device="cuda")
+    gates = torch.tensor([5, 399, 0, 17, 398, 5, 100, 250], dtype=torch.int32, device="cuda")
+    few, want = table(rng, (8, hidden), 1.0, "bf16").cuda(), torch.empty((8, hidden), dtype=torch.bfloat16, device="cuda")
+    dg4.dg4_sparse_attn_kv4_fwd(c, g, few, codes, scales, bias, want, ids=gates)
+    at = around(limit, rows)
+    ids = torch.full((rows,), -1, dtype=torch.int32, device="cuda")
+    Q = torch.full((rows, hidden), 7.0, dtype=torch.bfloat16, device="cuda")
+    ids[at], Q[at] = gates, few
+    A = torch.full_like(Q, 7.0)
+    call = lambda end: dg4.dg4_sparse_attn_kv4_fwd(c, g, Q, codes, scales, bias, A, ids=ids, row_end=end)
+    assert launches(lambda: call(limit)) == 1 and launches(lambda: call(limit + 1)) == 2
+    call(rows)
+    assert torch.equal(A[at], want)
+    A[at] = 7.0
+    assert torch.equal(A, A[1:2].expand_as(A))
+    # from a row that is not the first, in place
+    Q[at], A = few, None
+    dg4.dg4_sparse_attn_kv4_fwd(c, g, Q, codes, scales, bias, Q, ids=ids, row_begin=1)
+    assert torch.equal(Q[at[1:]], want[1:]) and torch.equal(Q[0], few[0])
+
+
+def test_write_and_read_in_several_launches():
+    """Rows of float at hidden 256, four of them to a workgroup: 2^25 to a launch."""
+    hidden, n, limit = 256, 64, 2 ** 25
+    rows = limit + 5
+    c = cfg(hidden, "f32")
+    print(f"kv4 write and read of {rows} rows, nearly all padding", flush=True)
+    at, gates = around(limit, rows), torch.tensor([5, 63, 0, 17, 31, 6, 40, 25], dtype=torch.int32, device="cuda")
+    few = table(np.random.default_rng(2), (8, hidden), 1.0, "f32")
+    ids = torch.full((rows,), -1, dtype=torch.int32, device="cuda")
+    K = torch.full((rows, hidden), 7.0, device="cuda")
+    ids[at], K[at] = gates, few.cuda()
+    codes = torch.full((n, hidden), 0x55, dtype=torch.uint8, device="cuda")
+    scales = torch.full((n, hidden // 32, 2), 0x66, dtype=torch.uint8, device="cuda")
+    write = lambda end: dg4.dg4_kv4_write(c, K, K, codes, scales, ids=ids, row_end=end)
+    assert launches(lambda: write(limit)) == 1 and launches(lambda: write(limit + 1)) == 2
+    write(rows)
+    code, byte = ref.store(to_np(few), to_np(few))
+    named = gates.cpu().numpy()
+    others = np.setdiff1d(np.arange(n), named)
+    got, at_scale = codes.cpu().numpy(), scales.cpu().numpy()
+    assert np.array_equal(got[named], code) and np.array_equal(at_scale[named], byte)
+    assert (got[others] == 0x55).all() and (at_scale[others] == 0x66).all()
+    K.fill_(7.0)
+    V = torch.full_like(K, 7.0)
+    read = lambda end: dg4.dg4_kv4_read(c, codes, scales, K, V, ids=ids, row_end=end)
+    assert launches(lambda: read(limit)) == 1 and launches(lambda: read(limit + 1)) == 2
+    read(rows)
+    for x, want in zip((K, V), ref.values(code, byte)):
+        assert torch.equal(x[at].cpu(), torch.from_numpy(want).float())
+        x[at] = 7.0
+        assert torch.equal(x, x[1:2].expand_as(x))
