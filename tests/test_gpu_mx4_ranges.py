@@ -1,4 +1,5 @@
-"""The calls in 4 bits at the ends of their ranges: calls of several launches."""
+"""The calls in 4 bits at the ends of their ranges: calls of several launches, the smallest keys, subnormal
+queries."""
 import ctypes
 import re
 
@@ -7,10 +8,15 @@ import pytest
 import torch
 
 import fp4_ref as ref
+import kv8_ref
 import paper_2502_01681_amd as dg4
+from fp4_ref import HALF_STEP
 from gpu_utils import tdtype, to_np
 
 pytestmark = pytest.mark.gpu
+
+SHAPES = [(128, "f32"), (256, "bf16"), (256, "f32"), (128, "bf16")]
+
 
 def cfg(hidden, dtype, hops=2, **kw):
     return dg4.LayerConfig(hidden, hidden // 32, hops, 1, dtype, **kw)
@@ -19,6 +25,11 @@ def cfg(hidden, dtype, hops=2, **kw):
 def table(rng, shape, size, dtype):
     """Normal numbers times size, rounded to the type, on the host."""
     return torch.from_numpy((rng.standard_normal(shape).clip(-3.5, 3.5) * size).astype(np.float32)).to(tdtype(dtype))
+
+
+def close(got, want, bound):
+    err = np.abs(got - want)
+    assert (err <= bound).all(), (err / bound).max()
 
 
 def launches(call):
@@ -101,3 +112,41 @@ def test_write_and_read_in_several_launches():
         assert torch.equal(x[at].cpu(), torch.from_numpy(want).float())
         x[at] = 7.0
         assert torch.equal(x, x[1:2].expand_as(x))
+
+
+def circuit(n, hops):
+    rng = np.random.default_rng(4)
+    fan = [(u, v, int(rng.integers(0, 2))) for v in range(8, n) for u in rng.choice(np.arange(max(0, v - 30), v), 2, replace=False)]
+    return dg4.dg4_build_levels(n, *(np.array(x) for x in zip(*fan)), hops)
+
+
+@pytest.mark.parametrize("hidden,dtype", SHAPES)
+@pytest.mark.parametrize("hops", [2, 5])
+@pytest.mark.parametrize("byte", [0, 252])
+def test_scores_of_the_smallest_and_the_largest_keys(hidden, dtype, hops, byte):
+    """Keys under the scale 2^-127 (subnormal in float) against Q about 2^125; keys under 2^125 against Q of normal numbers about 2^-125,
+    of these and one subnormal number to a head, and of subnormal numbers and zeros alone: ordinary scores, to which all of them count."""
+    n = 90
+    print(f"kv4 keys under 2^{byte - 127} {hidden} {dtype} hops={hops}", flush=True)
+    g = circuit(n, hops)
+    rng = np.random.default_rng(5)
+    codes = rng.integers(0, 256, (n, hidden)).astype(np.uint8)
+    scales = np.full((n, hidden // 32, 2), 126, dtype=np.uint8)
+    scales[:, :, 0] = byte
+    K, V = ref.values(codes, scales)
+    assert (K != 0).mean() > 0.8
+    if byte == 0:
+        q = rng.standard_normal((n, hidden)).clip(-3.5, 3.5) * 2.0 ** 125
+    else:
+        sign = np.where(rng.random((n, hidden)) < 0.5, 1.0, -1.0)
+        q = sign * (1 + rng.random((n, hidden))) * 2.0 ** -125
+        q[1::3, 9::32] = 3 * 2.0 ** -128
+        q[2::3] = sign[2::3] * rng.integers(0, 8, q[2::3].shape) * 2.0 ** -129
+    Q = torch.from_numpy(q).to(torch.float32).to(tdtype(dtype))
+    assert (Q != 0).float().mean() > 0.8
+    bias = rng.standard_normal((hidden // 32, 4)).astype(np.float32)
+    want, bound = kv8_ref.attention(g.array("nbr_ptr"), g.array("nbr_idx"), g.array("nbr_rel"), range(n), to_np(Q), K, V, bias, HALF_STEP[dtype])
+    A = torch.zeros((n, hidden), dtype=tdtype(dtype), device="cuda")
+    dev = lambda x: torch.from_numpy(x).cuda()
+    dg4.dg4_sparse_attn_kv4_fwd(cfg(hidden, dtype, hops), g, Q.cuda(), dev(codes), dev(scales), dev(bias), A)
+    close(to_np(A), want, bound)
