@@ -1,5 +1,5 @@
-"""The calls in 4 bits at the ends of their ranges: calls of several launches, the smallest keys, subnormal
-queries."""
+"""The calls in 4 bits at the ends of their ranges: calls of several launches, keys, rows and weights at the
+smallest scales, subnormal queries."""
 import ctypes
 import re
 
@@ -150,3 +150,56 @@ def test_scores_of_the_smallest_and_the_largest_keys(hidden, dtype, hops, byte):
     dev = lambda x: torch.from_numpy(x).cuda()
     dg4.dg4_sparse_attn_kv4_fwd(cfg(hidden, dtype, hops), g, Q.cuda(), dev(codes), dev(scales), dev(bias), A)
     close(to_np(A), want, bound)
+
+
+def lowest(x, axis):
+    """Whether all blocks of x along an axis are under 2^-127, and most of their codes are no zero."""
+    code, byte = ref.quantise(np.moveaxis(to_np(x).astype(np.float64), axis, -1))
+    return (byte == 0).all() and (code & 7 != 0).mean() > 0.6
+
+
+# Sizes of rows and weights: one of them is under the scale 2^-127 whole, the other brings the products back
+LOW = 2.0 ** -127
+
+
+@pytest.mark.parametrize("hidden,dtype", SHAPES)
+@pytest.mark.parametrize("which", ["rows", "weights"])
+def test_projection_at_the_lowest_scales(hidden, dtype, which):
+    rows, d = 70, hidden
+    print(f"mx4 projection, {which} under 2^-127 {hidden} {dtype}", flush=True)
+    rng = np.random.default_rng(6)
+    S = table(rng, (rows, d), LOW if which == "rows" else 2.0 ** 100, dtype)
+    W = table(rng, (d, 3 * d), LOW if which == "weights" else 2.0 ** 100, dtype)
+    assert lowest(S, 1) if which == "rows" else lowest(W, 0)
+    assert ref.exact_sums(to_np(S), to_np(W))
+    c = cfg(d, dtype)
+    packed, x = dg4.dg4_mx4_pack(c, W.cuda()), S.cuda()
+    out = [torch.zeros_like(x) for _ in range(3)]
+    dg4.dg4_qkv_proj_mx4(c, packed, x, *out)
+    y, bound = ref.proj(to_np(S), to_np(W), HALF_STEP[dtype])
+    close(np.concatenate([to_np(t) for t in out], 1), y, bound)
+    codes, scales = torch.zeros((rows, d), dtype=torch.uint8, device="cuda"), torch.zeros((rows, d // 32, 2), dtype=torch.uint8, device="cuda")
+    Q = torch.zeros_like(x)
+    dg4.dg4_qkv_proj_kv4(c, packed, x, Q, codes, scales)
+    code, byte = ref.store(y[:, d:2 * d], y[:, 2 * d:])
+    assert torch.equal(Q, out[0]) and np.array_equal(scales.cpu().numpy(), byte)
+    assert all(np.array_equal(a, b) for a, b in zip(ref.values(codes.cpu().numpy(), byte), ref.values(code, byte)))
+
+
+@pytest.mark.parametrize("hidden,dtype", SHAPES)
+@pytest.mark.parametrize("which,sizes", [("rows", (LOW, 2.0 ** 100, 1.0)), ("first weights", (2.0 ** 50, LOW, 2.0 ** 118)), ("second weights", (1.0, 2.0 ** 118, LOW))])
+def test_feed_forward_at_the_lowest_scales(hidden, dtype, which, sizes):
+    """Sums in which the product counts at least as much as a tenth of the row does, and a row's variance without an epsilon."""
+    rows, d = 50, hidden
+    print(f"mx4 feed-forward, {which} under 2^-127 {hidden} {dtype}", flush=True)
+    rng = np.random.default_rng(7)
+    S, W1, W2 = (table(rng, shape, size, dtype) for shape, size in zip(((rows, d), (d, 4 * d), (4 * d, d)), sizes))
+    assert lowest(S, 1) if which == "rows" else lowest(W1 if which == "first weights" else W2, 0)
+    h = np.maximum(ref.rounded(to_np(S)) @ ref.across(to_np(W1)), 0)
+    assert ref.exact_sums(to_np(S), to_np(W1)) and ref.exact_sums(h, to_np(W2))
+    assert np.linalg.norm(ref.rounded(h) @ ref.across(to_np(W2))) > 0.1 * np.linalg.norm(to_np(S).astype(np.float64))
+    c = cfg(d, dtype, ln_eps=0.0)
+    x = S.cuda()
+    out = torch.zeros_like(x)
+    dg4.dg4_ffn_mx4_fwd(c, dg4.dg4_mx4_pack(c, W1.cuda()), dg4.dg4_mx4_pack(c, W2.cuda()), x, out)
+    close(to_np(out), *ref.ffn(to_np(S), to_np(W1), to_np(W2), 0.0, HALF_STEP[dtype]))
