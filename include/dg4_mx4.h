@@ -22,7 +22,8 @@ extern "C" {
  * by it goes to the nearest code, ties to even, from 6 on to 6. Nothing else is rounded. The error of a
  * value is at most a fifth of it, or a fourteenth of the block's largest magnitude where that is more (or
  * 2^-129); over a block of normal numbers it is a ninth in the 2-norm. A block that holds an infinity or
- * a NaN gets byte 255 and stands for NaN.
+ * a NaN gets byte 255 and stands for NaN. Magnitudes above 1.75 * 2^127, an eighth below float's largest, go to
+ * 4 * 2^126 = 2^128, which the products take as it is and float and bfloat16 read as an infinity.
  *
  * The K|V store in 4 bits: the historical K and V rows (Section 3.4) in 272 bytes where hidden is 256, a
  * quarter of bfloat16's. A head (32 features) of K or V is a block. Store row u, n_store rows, device memory of

@@ -1,5 +1,5 @@
-"""The calls in 4 bits at the ends of their ranges: calls of several launches, keys, rows and weights at the
-smallest scales, subnormal queries."""
+"""The calls in 4 bits at the ends of their ranges: calls of several launches, keys, rows and weights at the smallest scales, subnormal
+queries, magnitudes that the type's largest number is below."""
 import ctypes
 import re
 
@@ -203,3 +203,20 @@ def test_feed_forward_at_the_lowest_scales(hidden, dtype, which, sizes):
     out = torch.zeros_like(x)
     dg4.dg4_ffn_mx4_fwd(c, dg4.dg4_mx4_pack(c, W1.cuda()), dg4.dg4_mx4_pack(c, W2.cuda()), x, out)
     close(to_np(out), *ref.ffn(to_np(S), to_np(W1), to_np(W2), 0.0, HALF_STEP[dtype]))
+
+
+@pytest.mark.parametrize("hidden,dtype", SHAPES)
+def test_magnitudes_that_the_type_does_not_reach(hidden, dtype):
+    """From 1.75 * 2^127 on a block's largest magnitudes go to 4 * 2^126, which float and bfloat16 read as an infinity; up to there to
+    6 * 2^125. The rest of the block reads as it is."""
+    x = torch.zeros((2, hidden))
+    x[0, 0], x[1, 0] = torch.finfo(tdtype(dtype)).max, 1.75 * 2.0 ** 127
+    x[:, 1], x[:, 40] = -2.0 ** 126, 3.0
+    x = x.to(tdtype(dtype)).cuda()
+    codes, scales = torch.zeros((2, hidden), dtype=torch.uint8, device="cuda"), torch.zeros((2, hidden // 32, 2), dtype=torch.uint8, device="cuda")
+    dg4.dg4_kv4_write(cfg(hidden, dtype), x, -x, codes, scales)
+    K, V = torch.ones_like(x), torch.ones_like(x)
+    dg4.dg4_kv4_read(cfg(hidden, dtype), codes, scales, K, V)
+    assert scales[:, 0, 0].tolist() == [253, 252] and torch.equal(K, -V)
+    assert K[0, 0] == np.inf and K[1, 0].float() == 1.5 * 2.0 ** 127
+    assert torch.equal(K[:, 1:], x[:, 1:])
