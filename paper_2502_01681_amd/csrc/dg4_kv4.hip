@@ -126,8 +126,11 @@ __device__ uint16_t dg4_raw_buffer_load2(dg4_i32x4 rsrc, int voffset, int soffse
 // A head's 32 values of q in a lane, and their product with the 32 codes of a source's K, which the conversions multiply by their
 // power of two (0: 2^-127, 255: NaN). fp32: value by value. bfloat16: as pairs, two products and a sum in fp32 per instruction, which
 // takes what is below 2^-126 as zero. Values of K there cost a score nothing as long as |q| is at most 2^80 (32 * 2^-126 * 2^80), and values of
-// q there do not occur in rows that have none: rows with a |q| above 2^80 or below 2^-126 (a zero is one; rows of Q hold few) take
-// dot_exact, every product in fp32.
+// q there do not occur in rows that have none: rows with a |q| above 2^80 or below 2^-126 take dot_exact, every product in fp32.
+// A zero counts as below. Rows of a product in bfloat16 hold next to none, but of the rows of dg4_qkv_proj_mx4 and dg4_qkv_proj_kv4, sums of coarse
+// steps, one in four to six has one, and a wave that holds such a row goes both ways. Time with Q of the one and of the other (us): a million
+// rows of two hops at hidden 256 311 and 337 (at 128 170 and 176), 200,000 of three 97 and 135, 90,000 of four 83 and 118, 15,135 of eight
+// at 128 56 and 62. (In a zero's place either way has the same product.)
 constexpr uint32_t LARGE_Q = (127u + 80u) << 23;  // 2^80, as a float's bits
 constexpr uint32_t SMALL_Q = 1u << 23;            // 2^-126
 template <typename T> struct HeadQ;
@@ -438,8 +441,9 @@ int launch_read(const dg4_kv8_args& args, hipStream_t s)
 // holds three gates, of two hops seven, fifteen, ...; MOST: what a call's cones hold at most. Measured with 1, 2, 4, 8 groups a row in bfloat16 (us;
 // two entries a step): 90,000 rows of four hops at 256 80, 83, 92, 119, but 1000 at 128 12.5, 7.9, 5.4, 4.8; 60,000 of five hops at 128 60, 56, 55,
 // 61; 30,000 of six hops at 256 107, 89, 82, 84; 20,000 of seven hops at 128 106, 72, 56, 51 (sixteen: 52); 15,135 of eight hops at 128 153, 101,
-// 72, 61 (sixteen: 56). Three hops, in one go by two groups: 200,000 rows at 256 101 (one group with four entries a step 102), 1000 of fp32 5.6
-// (8.6).
+// 72, 61 (sixteen: 56). Three hops go in one go by two groups, for calls of few rows: 1000 of fp32 at 256 take 5.6 where one group with four
+// entries a step takes 8.6. Calls of many pay 5 to 8 % for it, or nothing: 200,000 rows of bfloat16 at 256 101 (one group 102), at 128 58.0 (53.7),
+// 60,000 of fp32 at 256 42.9 (40.7), 100,000 at 128 41.0 (37.6).
 template <typename T, int D, bool FAR, int MOST>
 int launch_attn_of(const dg4_kv8_attn_args& args, hipStream_t s)
 {

@@ -7,8 +7,9 @@
 //
 // Weights are the A operand of 32x32x64 products and rows the B operand, so that a lane's sixteen accumulators belong to one
 // row; operand row 8 a + 4 hi + b is column 16 hi + 4 a + b of a tile, so they are sixteen neighbouring columns, half a block.
-// A product of two codes has at most 6 bits and a power of two takes none: sums in fp32 are exact as long as the powers of two of a
-// row's and a column's blocks lie within some 2^8 of each other.
+// A product of two codes is a whole number of quarters, up to 144 of them, under the powers of two of its blocks. Sums of k of them in fp32
+// are exact where (largest by smallest power of two of the row) * (the same of the column) * 144 k is at most 2^24: with the two
+// ratios together up to 2^9 at k = 128, 2^8 at 256, 2^7 at 512 and 2^6 at 1024.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -286,9 +287,11 @@ __global__ __launch_bounds__(2 * D) void mx4_proj_kernel(dg4_mx4_proj_args p)
 // form the activations, a quarter of W1's columns each; the other four multiply the activations, which go through LDS in 4 bits, by a quarter of
 // W2's columns each, and normalise. Between two barriers the former are a tile ahead of the latter: vector instructions of the one
 // (rounding to 4 bits, LayerNorm) run beside products of the other.
-// A million rows of bfloat16 at hidden 256: 326 us, 3.2 PFLOP/s, where the bytes take 199 at the rate of a copy and the products 149 at that of
-// a loop of them. A turn of a tile is 4200 cycles of each SIMD: 64 products, which keep its matrix core for 35 cycles and its vector
-// instructions from being issued for 16, and 614 vector instructions of 4 cycles, 3480 cycles in all; the clock falls to 1.8 GHz under it.
+// A million rows of bfloat16 at hidden 256: 325 to 330 us here, 354 on another card, 3.2 and 3.0 PFLOP/s, where the bytes take 199 at the rate of a
+// copy and the products 149 at that of a loop of them; at 128 124 (bytes: 99). A turn of a tile is 4900 cycles (256; counted, with the start shared
+// out) at 1.85 GHz in calls one after the other. Vector instructions and the issue of products take 3310 of them, 64 products keep the
+// matrix core for 2040; for some 1600 a SIMD issues nothing: it has one wave of each role, of 254 and 355 vector instructions to a
+// tile, which meet at a barrier for every tile, and a fifth of the waves' cycles is waiting.
 // Eight waves that all do everything, an eighth of either matrix each, in step: 365 us (their products and vector instructions come at the same
 // time), with rows and residual from memory instead of LDS, so that waits for loads were waits for stores: 412, with three barriers to a
 // tile: 520. Half the waves in the opposite order need more registers than there are. The residual of bfloat16 added by products with a unit
