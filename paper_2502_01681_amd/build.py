@@ -5,6 +5,7 @@ import contextlib
 import fcntl
 import glob
 import hashlib
+import importlib.machinery
 import importlib.util
 import os
 import subprocess
@@ -45,7 +46,8 @@ def _marshal_path() -> str:
     for path in [os.path.join(_torch(), "version.py"), MARSHAL_SOURCE] + MARSHAL_HEADERS:
         with open(path, "rb") as f:
             digest.update(f.read())
-    return os.path.join(HERE, "_dg4_marshal-" + digest.hexdigest()[:12] + sysconfig.get_config_var("EXT_SUFFIX"))
+    # (the suffix not from sysconfig, whose first use is not for two threads at once)
+    return os.path.join(HERE, "_dg4_marshal-" + digest.hexdigest()[:12] + importlib.machinery.EXTENSION_SUFFIXES[0])
 
 
 def stale() -> bool:

@@ -1,10 +1,10 @@
 """Building the library and the binding's native part: without torch, and by several who need it at once. The compilers are stood in
 for by what writes files (no device)."""
+import importlib.machinery
 import importlib.util
 import os
 import subprocess
 import sys
-import sysconfig
 import time
 
 import pytest
@@ -116,7 +116,7 @@ def test_those_who_need_it_first_wait_for_one_build(tmp_path, what):
 
 def test_a_module_of_other_sources_or_another_torch_is_not_taken(tmp_path, monkeypatch):
     here = build._marshal_path()
-    assert here == build._marshal_path() and here.endswith(sysconfig.get_config_var("EXT_SUFFIX"))
+    assert here == build._marshal_path() and here.endswith(importlib.machinery.EXTENSION_SUFFIXES[0])
     header = tmp_path / "dg4_mx4.h"
     header.write_text("other")
     with monkeypatch.context() as m:
